@@ -290,6 +290,23 @@ catq_status catq_ternary_linear(const void* X, int64_t M, int64_t ldx, const uin
                                 const float* alpha, int64_t d_out, int64_t d_in, int32_t g,
                                 void* Y, catq_dtype y_dtype, int64_t ldy, hipStream_t stream);
 
+/* catq_ternary_linear_a8 -- the same layer on 8-bit activations (W1.58A8 as it
+ * is deployed: codes and one scale per token instead of bf16 values):
+ *   Y[m][n] = x_scale[m] * sum_j alpha[n][j] * sum_{k in group j} q[m][k] * T[n][k]
+ * The inner sums are exact integers; groups are added in fp32 in a fixed order
+ * (bitwise deterministic for a given shape).
+ *   q        int8 [M][ldq] codes as catq_aux_rmsnorm_quant and
+ *            catq_aux_act_quant8 write them with group = d_in (d_in <= ldq <= 2^24,
+ *            ldq % 16 == 0)
+ *   x_scale  fp32 [M]
+ *   packed, alpha, d_out, d_in, g, Y, y_dtype, ldy  as for catq_ternary_linear
+ * M = 0 is a no-op.  q and alpha 16-byte aligned, packed 8-byte, x_scale and Y
+ * 4-byte. */
+catq_status catq_ternary_linear_a8(const int8_t* q, int64_t M, int64_t ldq, const float* x_scale,
+                                   const uint8_t* packed, const float* alpha, int64_t d_out,
+                                   int64_t d_in, int32_t g, void* Y, catq_dtype y_dtype,
+                                   int64_t ldy, hipStream_t stream);
+
 /* Fused variants for the SwiGLU MLP of a decoder block (a4 and a8 with the
  * SwiGLU of a5 / a7 in the GEMM epilogue; same results as the unfused calls).
  *
@@ -345,6 +362,30 @@ catq_status catq_aux_rmsnorm_bwd(const void* x, catq_dtype x_dtype, const float*
 catq_status catq_aux_act_quant(const void* x, catq_dtype x_dtype, int64_t rows, int64_t n,
                                int64_t group, void* y, hipStream_t stream);
 
+/* The same quantizer with its codes as the output (W1.58A8 as deployed), and
+ * the norm and residual addition in front of it in one pass:
+ *   h = x + res                    (rounded to r_dtype and written to `sum`; h = x
+ *                                   without res)
+ *   xh = h / sqrt(mean(h^2) + eps) * weight     (fp32, not rounded; weight bf16 [n],
+ *                                   NULL for ones)
+ *   per group: scale = max|xh| / 127, q = round-half-even(xh / scale) within
+ *   +-127 (0 where scale = 0), y = bf16(q * scale)
+ * all in IEEE fp32.  A group that holds a NaN or an infinity gets a NaN scale
+ * and zero codes.  catq_aux_act_quant8 has no norm, residual or weight (xh = x):
+ * its codes stand for exactly the values of catq_aux_act_quant on finite x.
+ *   x       [rows][n] of x_dtype; res, sum [rows][n] of r_dtype (both NULL, or
+ *           res given and sum NULL or not); sum may be res, or x where the types agree
+ *   y       bf16 [rows][n], may be NULL;  q int8 [rows][n] and scale fp32
+ *           [rows][n/group], both NULL or neither (then y must be given)
+ * n <= 32768, n and group multiples of 8, group dividing n.  rows = 0 is a
+ * no-op.  x, res, weight, sum and y 16-byte aligned, q 8-byte, scale 4-byte. */
+catq_status catq_aux_rmsnorm_quant(const void* x, catq_dtype x_dtype, const void* res,
+                                   catq_dtype r_dtype, const void* weight, int64_t rows, int64_t n,
+                                   int64_t group, float eps, void* sum, void* y, int8_t* q,
+                                   float* scale, hipStream_t stream);
+catq_status catq_aux_act_quant8(const void* x, catq_dtype x_dtype, int64_t rows, int64_t n,
+                                int64_t group, int8_t* q, float* scale, hipStream_t stream);
+
 /* Attention geometry for the q/k/v buffer produced by the fused q|k|v linear. */
 typedef struct {
   int32_t batch, seq, n_q, n_kv, head_dim;
@@ -373,6 +414,110 @@ catq_status catq_aux_attention_fwd(const catq_attn_desc* a, const void* qkv, voi
 catq_status catq_aux_attention_bwd(const catq_attn_desc* a, const void* qkv, const void* o,
                                    const void* saved, const void* d_o, void* dqkv,
                                    void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Serving: a paged key/value cache held in 8 bits, and attention over it.
+ *
+ * The pool holds n_pages pages of page_size tokens for every kv head:
+ *   k        int8 [n_pages][n_kv][page_size][head_dim]
+ *   v        int8 [n_pages][n_kv][page_size/4][head_dim][4]   (token t of a page at
+ *            [t/4][.][t%4])
+ *   k_scale, v_scale  fp32 [n_pages][n_kv][page_size/scale_block]: one scale for
+ *            each scale_block consecutive tokens of a head; a code c stands for
+ *            c * scale
+ * A sequence is a row of page_table (its page ids in order) and its length.  A
+ * page id outside [0, n_pages) where a page is needed is no error: tokens on it
+ * are dropped by the append, read back as 0, and unseen by the attention.
+ */
+typedef struct {
+  int32_t n_q, n_kv;     /* query and kv heads; n_q a multiple of n_kv              */
+  int32_t head_dim;      /* 64, 128 or 256                                          */
+  int32_t page_size;     /* tokens of a page: 16, 32, 64, 128 or 256                */
+  int32_t scale_block;   /* tokens that share a scale: 1, or 16, 32, 64 or 128 up to
+                            page_size                                               */
+  int32_t n_pages;       /* pages of the pool                                       */
+  int32_t max_pages;     /* columns of a page table row                             */
+} catq_kv_desc;
+typedef struct {
+  int8_t* k;
+  int8_t* v;
+  float* k_scale;
+  float* v_scale;
+} catq_kv_cache;         /* 16-byte aligned                                         */
+/* The new tokens of a batch of sequences.  Rows cu_new[s] .. cu_new[s+1] - 1 of the
+ * token arrays belong to sequence s, at positions ctx_len[s], ctx_len[s] + 1, ...;
+ * rows from cu_new[n_seqs] on belong to none and are left as they are.  The three
+ * arrays are read by the kernels on the device; values out of range there read and
+ * write nothing out of bounds (rows past n_tokens, positions below 0 or past max_pages *
+ * page_size, and a sequence's tokens past max_new are left out). */
+typedef struct {
+  const int32_t* page_table;  /* [n_seqs][max_pages]                                */
+  const int32_t* cu_new;      /* [n_seqs + 1], non-decreasing from 0                */
+  const int32_t* ctx_len;     /* [n_seqs]: tokens before the new ones               */
+  int64_t n_tokens;           /* rows of the token arrays                           */
+  int32_t n_seqs;
+  int32_t max_new;            /* no sequence has more new tokens                    */
+  int32_t max_len;            /* no sequence is longer than this with them; at most
+                                 max_pages * page_size.  Sizes grids and workspaces */
+} catq_kv_batch;
+typedef struct {
+  const float* inv_freq;  /* fp32 [rot_dim/2]: pair i of position p turns by p * inv_freq[i]
+                             (formed in float64); any scaling of the frequencies for
+                             long contexts is in them.  NULL if rot_dim is 0          */
+  const void* q_weight;   /* bf16 [head_dim] gain of the q norm, NULL for ones        */
+  const void* k_weight;
+  int32_t rot_dim;        /* leading values of a head that rotate: a multiple of 16, 0 ..
+                             head_dim                                                 */
+  int32_t interleaved;    /* pairs (2i, 2i+1); 0: pairs (i, i + rot_dim/2)            */
+  int32_t qk_norm;        /* RMSNorm of every q and k head before the rotation        */
+  int32_t act_quant;      /* 1: q fake-quantized to 8 bits per (token, head) (W1.58A8) */
+  float rope_scale;       /* factor on the rotated values (1 for none)                */
+  float eps;              /* of the norms                                             */
+} catq_kv_prep;
+
+/*
+ * catq_aux_kv_append: new tokens' qkv [n_tokens][(n_q + 2 n_kv) head_dim] (bf16; q
+ * heads, k heads, v heads) -> q_out [n_tokens][n_q head_dim] (bf16, normed and
+ * rotated) and their K (normed and rotated) and V in the cache.  All in fp32 up to
+ * the one rounding of q_out and of the codes.  A scale block's scale is
+ * max|new values| / 127, or the scale it has if that is larger and the block holds
+ * tokens before ctx_len; those older tokens' codes become
+ * round-half-even(code * (old scale / new scale)) where the scale grows.  A block
+ * that receives a NaN or an infinity gets a NaN scale.  A block that receives tokens
+ * belongs to one sequence of the batch; pages can be shared otherwise.  Appending
+ * the same tokens again gives the same cache.
+ * catq_aux_kv_read: positions ctx_len[s] + i back as the bf16 values they stand for,
+ * k_out and v_out [n_tokens][n_kv head_dim] (either may be NULL).
+ * Every pointer 16-byte aligned.
+ */
+catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_cache* cache,
+                               const catq_kv_batch* batch, const catq_kv_prep* prep,
+                               const void* qkv, void* q_out, hipStream_t stream);
+catq_status catq_aux_kv_read(const catq_kv_desc* d, const catq_kv_cache* cache,
+                             const catq_kv_batch* batch, void* k_out, void* v_out,
+                             hipStream_t stream);
+
+/*
+ * catq_aux_paged_attention: softmax attention of the new tokens over the cache
+ * (which holds them too: append first).  Row i of sequence s sees positions 0 ..
+ * ctx_len[s] + i:  o = sum_j softmax_j(scale * q . k_j) v_j, query head h on kv head
+ * h / (n_q / n_kv).
+ *   q, o   bf16 [n_tokens][n_q head_dim]
+ *   lse    fp32 [n_tokens][n_q], log(sum_j exp(scale * q . k_j)) (NULL: not written)
+ * A row that sees nothing gives o = 0 and lse = -inf.  Products are taken on fp16
+ * operands (the codes are exact in them; q is scaled to its row's largest
+ * magnitude, and elements more than 2^14 below that lose bits; the probabilities
+ * round to 11 bits), sums and softmax statistics in fp32.  A v_scale
+ * below 2^-60 counts as 0, and one above 2^30 as NaN: rows that see it are NaN.  The context is split over workgroups where few rows
+ * are asked for; the workspace then holds their partial results: at least
+ * catq_paged_attention_workspace_bytes(d, batch) bytes (0: may be NULL), for one call at a
+ * time.  Deterministic for given sizes (n_seqs, n_tokens, max_new, max_len).
+ */
+size_t catq_paged_attention_workspace_bytes(const catq_kv_desc* d, const catq_kv_batch* batch);
+catq_status catq_aux_paged_attention(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                     const catq_kv_batch* batch, const void* q, float scale,
+                                     void* o, float* lse, void* workspace,
+                                     size_t workspace_bytes, hipStream_t stream);
 
 /* SwiGLU on gu [rows][2F] (gate | up): a = silu(gate) * up, [rows][F]. */
 catq_status catq_aux_swiglu_fwd(const void* gu, int64_t rows, int64_t F, void* a,

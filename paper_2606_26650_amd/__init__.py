@@ -12,7 +12,7 @@ import torch
 
 from . import _lib
 from ._lib import (BF16, F32, HARD, IDENTITY, SOFT, WS_LINEAR_BWD, WS_LOSS, AttnDesc, CatqError,
-                   LmstParams)
+                   KvBatch, KvCache, KvDesc, KvPrep, LmstParams)
 
 __all__ = [
     "catq_modulate_ternarize", "catq_fakeq_linear_fwd", "catq_fakeq_linear_bwd",
@@ -24,6 +24,9 @@ __all__ = [
     "catq_aux_swiglu_fwd", "catq_aux_swiglu_bwd", "catq_aux_moe_route",
     "catq_aux_moe_route_workspace_bytes", "catq_aux_moe_gather", "catq_aux_moe_combine",
     "catq_aux_moe_combine_bwd", "catq_aux_moe_scatter_add", "catq_aux_adamw", "catq_aux_add",
+    "catq_ternary_linear_a8", "catq_aux_rmsnorm_quant", "catq_aux_act_quant8", "catq_aux_kv_append",
+    "catq_aux_kv_read", "catq_aux_paged_attention", "catq_paged_attention_workspace_bytes",
+    "kv_desc", "kv_cache", "kv_batch", "kv_prep", "KvDesc", "KvCache", "KvBatch", "KvPrep",
     "lmst_params", "attn_desc", "IDENTITY", "SOFT", "HARD", "F32", "BF16", "CatqError",
     "LmstParams", "AttnDesc", "lib", "catq_trace_enable", "catq_trace_pause",
     "catq_trace_reset", "catq_trace_count", "catq_trace_get", "catq_trace_disable",
@@ -286,6 +289,208 @@ def catq_aux_adamw(p, grad, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, lo
 def catq_aux_add(a, b, y, stream=None):
     st = lib.catq_aux_add(_ptr(a), _ptr(b), _ptr(y), _dt(a), a.numel(), _stream(stream))
     _lib.check("catq_aux_add", st)
+
+
+# ------------------------------------------------------------------ serving
+#
+# The calls below take tensors as they are: a tensor of another dtype, shape or
+# layout than the call documents, or one on another device than the first, is a
+# TypeError or ValueError here, before the library sees a pointer.  They run on the
+# device of their tensors and, without ``stream``, on that device's current stream.
+
+def _want(t, name, dtype, shape=None, device=None, strided=False):
+    if t.dtype != dtype if not isinstance(dtype, tuple) else t.dtype not in dtype:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    if not t.is_contiguous() and not (strided and t.dim() == 2 and t.stride(1) == 1):
+        raise ValueError(f"{name}: must be contiguous")
+    if device is None:
+        if not t.is_cuda:
+            raise ValueError(f"{name}: must be on a GPU")
+    elif t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+    return t
+
+
+_ACT = (torch.bfloat16, torch.float32)
+
+
+def _run_on(device, stream, fn, name, *args):
+    if device.index == torch.cuda.current_device():
+        _lib.check(name, fn(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(device):
+            _lib.check(name, fn(*args, _stream(stream)))
+
+
+def _bytes(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def catq_aux_rmsnorm_quant(x, q=None, scale=None, res=None, weight=None, sum=None, y=None, group=None,
+                           eps=1e-6, stream=None):
+    """h = x + res (into ``sum``), RMSNorm with gain ``weight``, and its 8-bit codes q
+    with their scales [rows][n/group] (default: one per row), or their values y in
+    bf16, or both."""
+    _want(x, "x", _ACT)
+    n, dev = x.shape[-1], x.device
+    rows = x.numel() // n if n else 0
+    group = n if group is None else group
+    for t, name in ((res, "res"), (sum, "sum")):
+        if t is not None:
+            _want(t, name, _ACT, tuple(x.shape), dev)
+    if res is not None and sum is not None and res.dtype != sum.dtype:
+        raise TypeError(f"sum: dtype {sum.dtype}, expected {res.dtype}")
+    if weight is not None:
+        _want(weight, "weight", torch.bfloat16, (n,), dev)
+    if y is not None:
+        _want(y, "y", torch.bfloat16, tuple(x.shape), dev)
+    if q is not None:
+        _want(q, "q", torch.int8, tuple(x.shape), dev)
+    if scale is not None:
+        _want(scale, "scale", torch.float32, None, dev)
+        if group > 0 and scale.numel() != rows * (n // group):
+            raise ValueError(f"scale: {scale.numel()} values, expected {rows * (n // group)}")
+    _run_on(dev, stream, lib.catq_aux_rmsnorm_quant, "catq_aux_rmsnorm_quant", _ptr(x), _dt(x), _ptr(res),
+            BF16 if res is None else _dt(res), _ptr(weight), rows, n, group, eps, _ptr(sum), _ptr(y), _ptr(q),
+            _ptr(scale))
+
+
+def catq_aux_act_quant8(x, q, scale, group=None, stream=None):
+    """The 8-bit codes of every group of ``group`` consecutive values of x's rows
+    (default: the whole row) and their scales."""
+    _want(x, "x", _ACT)
+    n, dev = x.shape[-1], x.device
+    rows = x.numel() // n if n else 0
+    group = n if group is None else group
+    _want(q, "q", torch.int8, tuple(x.shape), dev)
+    _want(scale, "scale", torch.float32, None, dev)
+    if group > 0 and scale.numel() != rows * (n // group):
+        raise ValueError(f"scale: {scale.numel()} values, expected {rows * (n // group)}")
+    _run_on(dev, stream, lib.catq_aux_act_quant8, "catq_aux_act_quant8", _ptr(x), _dt(x), rows, n, group,
+            _ptr(q), _ptr(scale))
+
+
+def catq_ternary_linear_a8(q, x_scale, packed, alpha, Y, g=128, stream=None):
+    """Y = x_scale * q (alpha * T)^T from the 2-bit storage: codes q int8 [M][d_in]
+    (rows may be strided), x_scale fp32 [M], packed uint8 [d_out][d_in/4], alpha
+    fp32 [d_out][d_in/g], Y fp32 or bf16 [M][d_out] (rows may be strided)."""
+    _want(packed, "packed", torch.uint8)
+    dev = packed.device
+    d_out, d_in = packed.shape[0], packed.shape[1] * 4
+    M = q.shape[0]
+    _want(q, "q", torch.int8, (M, d_in), dev, strided=True)
+    _want(Y, "Y", _ACT, (M, d_out), dev, strided=True)
+    for t, name, n in ((x_scale, "x_scale", M), (alpha, "alpha", d_out * (d_in // g) if g > 0 else 0)):
+        _want(t, name, torch.float32, None, dev)
+        if g > 0 and t.numel() != n:
+            raise ValueError(f"{name}: {t.numel()} values, expected {n}")
+    _run_on(dev, stream, lib.catq_ternary_linear_a8, "catq_ternary_linear_a8", _ptr(q), M,
+            q.stride(0) if M > 1 else d_in, _ptr(x_scale), _ptr(packed), _ptr(alpha), d_out, d_in, g, _ptr(Y),
+            _dt(Y), Y.stride(0) if M > 1 else d_out)
+
+
+def kv_desc(n_q, n_kv, head_dim, page_size, scale_block, n_pages, max_pages):
+    """Geometry of a paged 8-bit cache (see catq_kv_desc in the header)."""
+    return KvDesc(n_q, n_kv, head_dim, page_size, scale_block, n_pages, max_pages)
+
+
+def kv_cache(desc, k, v, k_scale, v_scale):
+    """The pool's arrays: k int8 [n_pages][n_kv][page_size][head_dim], v int8
+    [n_pages][n_kv][page_size/4][head_dim][4], scales fp32
+    [n_pages][n_kv][page_size/scale_block].  The returned struct keeps them."""
+    d = desc
+    _want(k, "k", torch.int8, (d.n_pages, d.n_kv, d.page_size, d.head_dim))
+    _want(v, "v", torch.int8, (d.n_pages, d.n_kv, d.page_size // 4, d.head_dim, 4), k.device)
+    blocks = (d.n_pages, d.n_kv, d.page_size // d.scale_block if d.scale_block > 0 else 0)
+    _want(k_scale, "k_scale", torch.float32, blocks, k.device)
+    _want(v_scale, "v_scale", torch.float32, blocks, k.device)
+    c = KvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+    c.tensors, c.device, c.geometry = (k, v, k_scale, v_scale), k.device, bytes(d)[:24]
+    return c
+
+
+def kv_batch(desc, page_table, cu_new, ctx_len, n_tokens, max_new, max_len):
+    """The new tokens of a batch (see catq_kv_batch in the header): page_table int32
+    [n_seqs][max_pages], cu_new int32 [n_seqs + 1], ctx_len int32 [n_seqs], on the
+    device; their values may change between calls.  The returned struct keeps them."""
+    n = ctx_len.shape[0]
+    _want(page_table, "page_table", torch.int32, (n, desc.max_pages))
+    _want(cu_new, "cu_new", torch.int32, (n + 1,), page_table.device)
+    _want(ctx_len, "ctx_len", torch.int32, (n,), page_table.device)
+    b = KvBatch(page_table.data_ptr(), cu_new.data_ptr(), ctx_len.data_ptr(), n_tokens, n, max_new, max_len)
+    b.tensors, b.device = (page_table, cu_new, ctx_len), page_table.device
+    return b
+
+
+def kv_prep(desc, inv_freq=None, rot_dim=0, interleaved=False, qk_norm=False, q_weight=None, k_weight=None,
+            eps=1e-6, rope_scale=1.0, act_quant=False):
+    """What happens to q and k on the way to the cache (see catq_kv_prep in the
+    header).  The returned struct keeps the tensors."""
+    first = next((t for t in (inv_freq, q_weight, k_weight) if t is not None), None)
+    dev = None if first is None else first.device
+    if inv_freq is not None:
+        _want(inv_freq, "inv_freq", torch.float32, (rot_dim // 2,))
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None:
+            _want(t, name, torch.bfloat16, (desc.head_dim,), dev)
+    p = KvPrep(_ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), rot_dim, int(bool(interleaved)),
+               int(bool(qk_norm)), int(bool(act_quant)), rope_scale, eps)
+    p.tensors, p.device = (inv_freq, q_weight, k_weight), dev
+    return p
+
+
+def _kv_same(desc, cache, batch):
+    dev = cache.device
+    if batch.device != dev:
+        raise ValueError(f"batch: on {batch.device}, expected {dev}")
+    if bytes(desc)[:24] != cache.geometry:
+        raise ValueError("the cache was made for another descriptor")
+    if batch.tensors[0].shape[1] != desc.max_pages:
+        raise ValueError("the batch's page table is not max_pages wide")
+    return dev
+
+
+def catq_aux_kv_append(desc, cache, batch, prep, qkv, q_out, stream=None):
+    """New tokens' qkv [n_tokens][(n_q + 2 n_kv) head_dim] (bf16): normed and rotated
+    q into q_out [n_tokens][n_q head_dim], k and v into the cache."""
+    dev, n, d = _kv_same(desc, cache, batch), batch.n_tokens, desc.head_dim
+    if prep.device is not None and prep.device != dev:
+        raise ValueError(f"prep: on {prep.device}, expected {dev}")
+    _want(qkv, "qkv", torch.bfloat16, (n, (desc.n_q + 2 * desc.n_kv) * d), dev)
+    _want(q_out, "q_out", torch.bfloat16, (n, desc.n_q * d), dev)
+    _run_on(dev, stream, lib.catq_aux_kv_append, "catq_aux_kv_append", C.byref(desc), C.byref(cache),
+            C.byref(batch), C.byref(prep), _ptr(qkv), _ptr(q_out))
+
+
+def catq_aux_kv_read(desc, cache, batch, k_out=None, v_out=None, stream=None):
+    """The batch's positions back as bf16 values [n_tokens][n_kv head_dim]."""
+    dev, shape = _kv_same(desc, cache, batch), (batch.n_tokens, desc.n_kv * desc.head_dim)
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is not None:
+            _want(t, name, torch.bfloat16, shape, dev)
+    _run_on(dev, stream, lib.catq_aux_kv_read, "catq_aux_kv_read", C.byref(desc), C.byref(cache),
+            C.byref(batch), _ptr(k_out), _ptr(v_out))
+
+
+def catq_paged_attention_workspace_bytes(desc, batch):
+    return int(lib.catq_paged_attention_workspace_bytes(C.byref(desc), C.byref(batch)))
+
+
+def catq_aux_paged_attention(desc, cache, batch, q, o, workspace=None, scale=None, lse=None, stream=None):
+    """Attention of the new tokens' q over the cache that holds them (scale None:
+    1/sqrt(head_dim)); o like q, lse fp32 [n_tokens][n_q] or None."""
+    dev, shape = _kv_same(desc, cache, batch), (batch.n_tokens, desc.n_q * desc.head_dim)
+    _want(q, "q", torch.bfloat16, shape, dev)
+    _want(o, "o", torch.bfloat16, shape, dev)
+    if lse is not None:
+        _want(lse, "lse", torch.float32, (batch.n_tokens, desc.n_q), dev)
+    if workspace is not None and workspace.device != dev:
+        raise ValueError(f"workspace: on {workspace.device}, expected {dev}")
+    _run_on(dev, stream, lib.catq_aux_paged_attention, "catq_aux_paged_attention", C.byref(desc),
+            C.byref(cache), C.byref(batch), _ptr(q), desc.head_dim ** -0.5 if scale is None else scale, _ptr(o),
+            _ptr(lse), _ptr(workspace), _bytes(workspace))
 
 
 def catq_trace_enable(capacity):

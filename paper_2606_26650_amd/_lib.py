@@ -30,6 +30,27 @@ class AttnDesc(C.Structure):
                 ("rope_theta", C.c_float), ("eps", C.c_float), ("act_quant", C.c_int32)]
 
 
+class KvDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q", "n_kv", "head_dim", "page_size", "scale_block",
+                                         "n_pages", "max_pages")]
+
+
+class KvCache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class KvBatch(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("cu_new", C.c_void_p), ("ctx_len", C.c_void_p),
+                ("n_tokens", C.c_int64), ("n_seqs", C.c_int32), ("max_new", C.c_int32),
+                ("max_len", C.c_int32)]
+
+
+class KvPrep(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("qk_norm", C.c_int32),
+                ("act_quant", C.c_int32), ("rope_scale", C.c_float), ("eps", C.c_float)]
+
+
 class TraceRec(C.Structure):
     _fields_ = [("tag", C.c_char * 96), ("flops", C.c_double), ("bytes", C.c_double),
                 ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("ms", C.c_float)]
@@ -44,6 +65,7 @@ class CatqError(RuntimeError):
 P, I64, I32, F, SZ = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_size_t
 PP = C.POINTER(LmstParams)
 PA = C.POINTER(AttnDesc)
+PKD, PKC, PKB, PKP = (C.POINTER(s) for s in (KvDesc, KvCache, KvBatch, KvPrep))
 
 SIGNATURES = {
     "catq_modulate_ternarize": [P, I32, I64, I64, P, P, P, PP, P, I32, P, I32, P, P, P],
@@ -57,10 +79,17 @@ SIGNATURES = {
     "catq_fakeq_gateup_swiglu_fwd": [P, P, I64, I64, I64, P, P, P],
     "catq_fakeq_down_swiglu_bwd": [P, P, I64, I64, I64, P, P, P, P],
     "catq_ternary_linear": [P, I64, I64, P, P, I64, I64, I32, P, I32, I64, P],
+    "catq_ternary_linear_a8": [P, I64, I64, P, P, P, I64, I64, I32, P, I32, I64, P],
     "catq_workspace_size": [I32, I64, I64, I64, I32],
     "catq_status_string": [I32],
     "catq_last_error_message": [],
     "catq_aux_act_quant": [P, I32, I64, I64, I64, P, P],
+    "catq_aux_rmsnorm_quant": [P, I32, P, I32, P, I64, I64, I64, F, P, P, P, P, P],
+    "catq_aux_act_quant8": [P, I32, I64, I64, I64, P, P, P],
+    "catq_aux_kv_append": [PKD, PKC, PKB, PKP, P, P, P],
+    "catq_aux_kv_read": [PKD, PKC, PKB, P, P, P],
+    "catq_paged_attention_workspace_bytes": [PKD, PKB],
+    "catq_aux_paged_attention": [PKD, PKC, PKB, P, F, P, P, P, SZ, P],
     "catq_aux_rmsnorm_fwd": [P, I32, I64, I64, F, P, P, P],
     "catq_aux_rmsnorm_bwd": [P, I32, P, P, P, I64, I64, P, P],
     "catq_attn_saved_bytes": [PA],
@@ -87,6 +116,7 @@ SIGNATURES = {
 RESTYPES = {"catq_workspace_size": SZ, "catq_status_string": C.c_char_p,
             "catq_last_error_message": C.c_char_p, "catq_attn_saved_bytes": SZ,
             "catq_attn_bwd_workspace_bytes": SZ, "catq_aux_moe_route_workspace_bytes": SZ,
+            "catq_paged_attention_workspace_bytes": SZ,
             "catq_trace_pause": None, "catq_trace_reset": None, "catq_trace_disable": None}
 
 _lib = None

@@ -19,7 +19,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcatq.so")
 
 SOURCES = ["status.hip", "trace.hip", "lmst.hip", "gemm.hip", "linear.hip", "loss.hip", "glue.hip",
-           "attention.hip", "flash.hip", "ternary.hip"]
+           "attention.hip", "flash.hip", "ternary.hip", "ternary_a8.hip", "norm_quant.hip", "kv_cache.hip",
+           "paged_attn.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
@@ -27,10 +28,11 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
          "-I", INCLUDE, "-I", CSRC, "-Wall", "-Wno-unused-result"]
 
 
-# per-source code generation options: the packed-ternary product keeps its
-# matrix-core accumulators in ordinary VGPRs (it scales them after every
+# per-source code generation options: the packed-ternary products keep their
+# matrix-core accumulators in ordinary VGPRs (they scale them after every
 # 128-code chunk, so accumulation registers would cost a copy each time)
-EXTRA = {"ternary.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA = {"ternary.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "ternary_a8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> str:

@@ -1,0 +1,507 @@
+// The paged 8-bit key/value cache (gfx950): new tokens in, with the head norms and
+// the rotation on the way, and values back out.
+//
+// Append.  One launch, two kinds of workgroups:
+//  * q: a workgroup takes one token and as many query heads as 256 threads cover
+//    at eight values each; its rotation angles are formed once in LDS.
+//  * k and v: a workgroup takes a window of W tokens of one kv head of K or V, W the
+//    larger of a scale block and what 256 threads cover (16 tokens of 128), so it
+//    owns whole scale blocks and whole four-token words of the v layout: no other
+//    workgroup reads or writes them.  It keeps the window's values in registers
+//    (eight per thread and pass of 256 threads), reduces their magnitudes to the blocks'
+//    scales through LDS, and writes codes (v through a transposed LDS tile, so that
+//    four tokens make one word).  Where a block holds older tokens and its scale
+//    grows, their codes are read, rescaled and written with the new ones.
+// A few new tokens cost a launch and two memory latencies; many are HBM bound.
+//
+// Angles are taken in float64: position * inv_freq reaches 1e6 radians, where a
+// product in fp32 is off by 0.06; the fraction of a turn is then exact to 1e-10 and
+// its sine and cosine are fp32.
+#include <type_traits>
+
+#include "kv_common.h"
+#include "quant8.h"
+
+namespace catq {
+
+catq_status kv_check_sizes(const catq_kv_desc* d, const catq_kv_batch* b) {
+  CATQ_REQUIRE(d && b, CATQ_ERR_NULL, "descriptor and batch must not be NULL");
+  CATQ_REQUIRE(d->n_q > 0 && d->n_kv > 0 && d->n_q % d->n_kv == 0 && d->n_q <= 1024,
+               CATQ_ERR_SHAPE, "n_q must be a multiple of n_kv and at most 1024");
+  CATQ_REQUIRE(d->head_dim == 64 || d->head_dim == 128 || d->head_dim == 256, CATQ_ERR_SHAPE,
+               "head_dim must be 64, 128 or 256");
+  const int ps = d->page_size, bt = d->scale_block;
+  CATQ_REQUIRE(ps >= 16 && ps <= 256 && (ps & (ps - 1)) == 0, CATQ_ERR_SHAPE,
+               "page_size must be 16, 32, 64, 128 or 256");
+  CATQ_REQUIRE(bt == 1 || (bt >= 16 && bt <= 128 && bt <= ps && (bt & (bt - 1)) == 0),
+               CATQ_ERR_SHAPE, "scale_block must be 1, or 16, 32, 64 or 128 and at most page_size");
+  CATQ_REQUIRE(d->n_pages > 0 && d->max_pages > 0 &&
+                   count_ok((int64_t)d->n_pages * ps, d->n_kv, d->head_dim),
+               CATQ_ERR_SHAPE, "n_pages and max_pages must be > 0, the pool within 2^38 elements");
+  CATQ_REQUIRE(b->n_seqs >= 0 && b->n_tokens >= 0 && b->max_new >= 0 && b->max_len >= 0,
+               CATQ_ERR_SHAPE, "batch sizes must be >= 0");
+  CATQ_REQUIRE(b->n_tokens <= INT32_MAX && b->n_seqs <= 65535 && b->max_new <= (1 << 24),
+               CATQ_ERR_SHAPE, "at most 2^31 - 1 tokens, 65535 sequences and 2^24 new tokens in one");
+  CATQ_REQUIRE(b->max_len <= (int64_t)d->max_pages * ps, CATQ_ERR_SHAPE,
+               "max_len exceeds what max_pages pages hold");
+  CATQ_REQUIRE(b->n_tokens == 0 ||
+                   count_ok(b->n_tokens, d->n_q + 2 * (int64_t)d->n_kv, d->head_dim),
+               CATQ_ERR_SHAPE, "too many tokens (more than 2^38 elements)");
+  return CATQ_OK;
+}
+
+catq_status kv_check(const catq_kv_desc* d, const catq_kv_cache* c, const catq_kv_batch* b) {
+  CATQ_TRY(kv_check_sizes(d, b));
+  CATQ_REQUIRE(c && c->k && c->v && c->k_scale && c->v_scale, CATQ_ERR_NULL, "cache arrays must not be NULL");
+  CATQ_REQUIRE(b->n_seqs == 0 || (b->page_table && b->cu_new && b->ctx_len), CATQ_ERR_NULL,
+               "batch arrays must not be NULL");
+  CATQ_REQUIRE(aligned16(c->k) && aligned16(c->v) && aligned16(c->k_scale) && aligned16(c->v_scale),
+               CATQ_ERR_ALIGN, "cache arrays must be 16-byte aligned");
+  CATQ_REQUIRE(((reinterpret_cast<uintptr_t>(b->page_table) | reinterpret_cast<uintptr_t>(b->cu_new) |
+                 reinterpret_cast<uintptr_t>(b->ctx_len)) & 3) == 0,
+               CATQ_ERR_ALIGN, "batch arrays must be 4-byte aligned");
+  return CATQ_OK;
+}
+
+KvGeom kv_geom(const catq_kv_desc* d, const catq_kv_batch* b) {
+  return KvGeom{b->page_table, b->cu_new, b->ctx_len, b->n_tokens, d->n_q, d->n_kv, d->head_dim,
+                __builtin_ctz((unsigned)d->page_size), __builtin_ctz((unsigned)d->scale_block),
+                d->n_pages, d->max_pages, b->n_seqs, b->max_new};
+}
+
+namespace {
+
+struct AppendArgs {
+  KvGeom g;
+  catq_kv_cache c;
+  const float* inv_freq;
+  const bf16* q_w;
+  const bf16* k_w;
+  const bf16* qkv;
+  bf16* q_out;
+  int32_t rot, inter, qk_norm, act_quant;
+  float rope_scale, eps;
+  int32_t win;          // windows a sequence can reach
+  int32_t w_log2;       // tokens of a window
+  int64_t kv_blocks;    // n_seqs * win * n_kv * 2 workgroups come first
+  int32_t q_parts;      // workgroups per token for the query heads
+};
+
+// cos and sin of `n` consecutive positions from pos0, [token][rot/2], times the scale
+__device__ __forceinline__ void angles(const AppendArgs& a, int64_t pos0, int n, float2* cs, int nt) {
+  const int half = a.rot >> 1;
+  for (int i = threadIdx.x; i < n * half; i += nt) {
+    const int t = i / half, f = i - t * half;
+    // in half turns: the fraction is what counts
+    const double turn = (double)(pos0 + t) * (double)a.inv_freq[f] * 0.31830988618379067154;
+    const float r = (float)(turn - 2.0 * rint(turn * 0.5));
+    float s, c;
+    sincospif(r, &s, &c);
+    cs[i] = make_float2(c * a.rope_scale, s * a.rope_scale);
+  }
+}
+
+// Eight values of a head held by lane `sub` of LPH: norm (with its gain) and rotation.
+template <int LPH>
+__device__ __forceinline__ void prep_head(const AppendArgs& a, float (&v)[8], int sub, const bf16* w,
+                                          const float2* cs) {
+  constexpr int D = LPH * 8;
+  if (a.qk_norm) {
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fmaf(v[j], v[j], ss);
+#pragma unroll
+    for (int m = LPH >> 1; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, 64);
+    const float r = 1.0f / sqrtf(ss / (float)D + a.eps);
+    if (w) {
+      float g[8];
+      load8<bf16>(w + sub * 8, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = v[j] * r * g[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= r;
+    }
+  }
+  if (a.rot == 0) return;
+  const int lanes = a.rot >> 3;   // lanes that rotate
+  if (a.inter) {
+    if (sub < lanes) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 t = cs[sub * 4 + j];
+        const float x = v[2 * j], y = v[2 * j + 1];
+        v[2 * j] = x * t.x - y * t.y;
+        v[2 * j + 1] = y * t.x + x * t.y;
+      }
+    }
+    return;
+  }
+  const int hl = lanes >> 1;      // lanes of the first half
+  const int lane = threadIdx.x & 63, base = lane - sub;
+  const int other = sub < hl ? sub + hl : sub < lanes ? sub - hl : sub;
+  float p[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) p[j] = __shfl(v[j], base + other, 64);
+  if (sub < lanes) {
+    const int f0 = (sub < hl ? sub : other) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 t = cs[f0 + j];
+      v[j] = sub < hl ? v[j] * t.x - p[j] * t.y : v[j] * t.x + p[j] * t.y;
+    }
+  }
+}
+
+template <int LPH>
+__device__ __forceinline__ void append_q(const AppendArgs& a, int64_t block, float2* cs, int* s_seq) {
+  constexpr int D = LPH * 8, HP = 256 / LPH;   // heads per workgroup
+  const int64_t t = block / a.q_parts;
+  const int part = (int)(block % a.q_parts);
+  // the token's sequence: the last one that starts at or before it (empty ones
+  // before it start there too)
+  if (threadIdx.x == 0) {
+    int lo = 0, hi = a.g.n_seqs;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.g.cu[mid] <= t) lo = mid; else hi = mid;
+    }
+    *s_seq = lo;
+  }
+  __syncthreads();
+  const KvSeq q = kv_seq(a.g, *s_seq);
+  if (t < q.row0 || t >= q.row0 + q.n) return;   // a row of no sequence
+  const int64_t pos = q.ctx + (t - q.row0);
+  angles(a, pos, 1, cs, 256);
+  __syncthreads();
+  const int sub = threadIdx.x & (LPH - 1), h = part * HP + threadIdx.x / LPH;
+  const bool live = h < a.g.n_q;
+  float v[8];
+  if (live)
+    load8<bf16>(a.qkv + t * (a.g.n_q + 2 * (int64_t)a.g.n_kv) * D + (int64_t)h * D + sub * 8, v);
+  else
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+  prep_head<LPH>(a, v, sub, a.q_w, cs);
+  if (a.act_quant) {
+    unsigned int m = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, mag_bits(v[j]));
+#pragma unroll
+    for (int k = LPH >> 1; k >= 1; k >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, k, 64));
+    const float s = quant8_scale(m);
+    const Quant8 quant(s);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = quant(v[j]) * s;
+  }
+  if (live) store8<bf16>(a.q_out + (t * a.g.n_q + h) * D + sub * 8, v);
+}
+
+// byte b of a word as a signed code
+__device__ __forceinline__ float code_of(unsigned int w, int b) {
+  return (float)(int)(signed char)(w >> (8 * b));
+}
+
+// LPH lanes per head, NP passes of TP = 256 / LPH tokens (or one of fewer)
+template <int LPH, int NP>
+__device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, float2* cs,
+                                          unsigned int* s_mag, float* s_scale, float* s_ratio,
+                                          unsigned char* s_tile) {
+  constexpr int D = LPH * 8, TP = 256 / LPH;
+  const KvGeom& g = a.g;
+  const int is_v = (int)(block & 1);
+  block >>= 1;
+  const int h = (int)(block % g.n_kv);
+  block /= g.n_kv;
+  const int wi = (int)(block % a.win), s = (int)(block / a.win);
+  const KvSeq q = kv_seq(g, s);
+  const int W = 1 << a.w_log2;
+  // positions first <= p < first + W of the window, of which lo <= p < hi are new
+  const int64_t begin = q.ctx < 0 ? 0 : q.ctx;
+  const int64_t first = ((begin >> a.w_log2) + wi) << a.w_log2;
+  const int64_t end = min((int64_t)q.ctx + q.n, kv_capacity(g));
+  if (first >= end || begin >= end) return;
+  const int page = g.table[(int64_t)s * g.max_pages + (first >> g.ps_log2)];
+  if (page < 0 || page >= g.n_pages) return;
+  const int tok0 = (int)(first & ((1 << g.ps_log2) - 1));   // of the page
+  const int lo = (int)max(begin - first, (int64_t)0), hi = (int)min(end - first, (int64_t)W);
+  const int bt = 1 << g.bt_log2;
+  // the block with older tokens, if there is one: [lo & ~(bt-1), lo) hold them
+  const int old0 = lo & ~(bt - 1);
+  const bool has_old = first + lo == begin && old0 < lo;
+
+  const int sub = threadIdx.x & (LPH - 1), tl = threadIdx.x / LPH;
+  const int64_t ld = (g.n_q + 2 * (int64_t)g.n_kv) * D;
+  const bf16* src = a.qkv + (int64_t)(g.n_q + (is_v ? g.n_kv : 0) + h) * D + sub * 8;
+  float v[NP][8];
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const int t = p * TP + tl;
+    if (t >= lo && t < hi) {
+      load8<bf16>(src + (q.row0 + (first + t - q.ctx)) * ld, v[p]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[p][j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const int t = p * TP + tl;
+    if (!is_v) {
+      if (p > 0) __syncthreads();   // the table of the pass before is read
+      if (p * TP < hi && (p + 1) * TP > lo) angles(a, first + p * TP, TP, cs, 256);
+      __syncthreads();
+      prep_head<LPH>(a, v[p], sub, a.k_w, cs + tl * (a.rot >> 1));
+      if (t < lo || t >= hi)        // (a norm turns zeros into zeros, an angle may be anything)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[p][j] = 0.f;
+    }
+    unsigned int m = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, mag_bits(v[p][j]));
+#pragma unroll
+    for (int k = LPH >> 1; k >= 1; k >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, k, 64));
+    if (sub == 0 && t < W) s_mag[t] = m;
+  }
+  __syncthreads();
+  float* scales = is_v ? a.c.v_scale : a.c.k_scale;
+  int8_t* codes = is_v ? a.c.v : a.c.k;
+  const int64_t cbase = kv_code_base(g, page, h, tok0);
+  const int64_t sbase = kv_scale_index(g, page, h, tok0);
+  for (int b = threadIdx.x; b < (W >> g.bt_log2); b += 256) {
+    const int t0 = b << g.bt_log2;
+    if (t0 >= hi || t0 + bt <= lo) continue;
+    unsigned int m = 0u;
+    for (int i = 0; i < bt; ++i) m = max(m, s_mag[t0 + i]);
+    float sc = quant8_scale(m), ratio = 1.0f;
+    if (has_old && t0 == old0) {
+      const float was = scales[sbase + b];
+      if (sc > was) ratio = was / sc;
+      else if (!(sc != sc)) sc = was;    // the larger; a NaN in either stays
+      if (sc != sc) ratio = 1.0f;
+      s_ratio[0] = ratio;
+    }
+    scales[sbase + b] = sc;
+    s_scale[b] = sc;
+  }
+  __syncthreads();
+  const bool grew = has_old && s_ratio[0] != 1.0f;
+  const int wlo = grew ? old0 : lo;   // tokens wlo .. hi - 1 are written
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const int t = p * TP + tl;
+    if (t < wlo || t >= hi) continue;
+    unsigned int c0, c1;
+    if (t < lo) {   // an older token of the block whose scale grew
+      const float r = s_ratio[0];
+      float o[8];
+      if (is_v) {
+        const int8_t* vp = codes + cbase + (int64_t)(t >> 2) * (4 * D) + sub * 32 + (t & 3);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = rintf((float)vp[4 * j] * r);
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(codes + cbase + (int64_t)t * D + sub * 8);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          o[j] = rintf(code_of(w.x, j) * r);
+          o[4 + j] = rintf(code_of(w.y, j) * r);
+        }
+      }
+      c0 = pack_codes(o[0], o[1], o[2], o[3]);
+      c1 = pack_codes(o[4], o[5], o[6], o[7]);
+    } else {
+      const Quant8 quant(s_scale[t >> g.bt_log2]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[p][j] = quant(v[p][j]);
+      c0 = pack_codes(v[p][0], v[p][1], v[p][2], v[p][3]);
+      c1 = pack_codes(v[p][4], v[p][5], v[p][6], v[p][7]);
+    }
+    if (is_v)
+      *reinterpret_cast<uint2*>(s_tile + t * D + sub * 8) = make_uint2(c0, c1);
+    else
+      *reinterpret_cast<uint2*>(codes + cbase + (int64_t)t * D + sub * 8) = make_uint2(c0, c1);
+  }
+  if (!is_v) return;
+  __syncthreads();
+  // words of four tokens at one d, whole ones at once and the others by bytes
+  for (int i = threadIdx.x; i < (W >> 2) * D; i += 256) {
+    const int t4 = (i / D) * 4, dd = i % D;
+    if (t4 + 4 <= wlo || t4 >= hi) continue;
+    int8_t* dst = codes + cbase + (int64_t)t4 * D + dd * 4;
+    if (t4 >= wlo && t4 + 4 <= hi) {
+      *reinterpret_cast<unsigned int*>(dst) =
+          (unsigned)s_tile[t4 * D + dd] | ((unsigned)s_tile[(t4 + 1) * D + dd] << 8) |
+          ((unsigned)s_tile[(t4 + 2) * D + dd] << 16) | ((unsigned)s_tile[(t4 + 3) * D + dd] << 24);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (t4 + k >= wlo && t4 + k < hi) dst[k] = (int8_t)s_tile[(t4 + k) * D + dd];
+    }
+  }
+}
+
+template <int LPH, int NP>
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
+  constexpr int D = LPH * 8, TP = 256 / LPH;
+  __shared__ float2 cs[TP * D / 2];
+  __shared__ unsigned int s_mag[TP * NP];
+  __shared__ float s_scale[TP * NP];
+  __shared__ float s_ratio[1];
+  __shared__ int s_seq;
+  __shared__ __align__(16) unsigned char s_tile[TP * NP * D];
+  const int64_t b = blockIdx.x;
+  if (b < a.kv_blocks)
+    append_kv<LPH, NP>(a, b, cs, s_mag, s_scale, s_ratio, s_tile);
+  else
+    append_q<LPH>(a, b - a.kv_blocks, cs, &s_seq);
+}
+
+// Eight values of one (token, head) per thread.  A v word holds four tokens: the
+// thread reads the 32 bytes of its eight words and takes its token's (the other three
+// tokens' threads find them in the cache).
+__global__ __launch_bounds__(256) void kv_read_kernel(KvGeom g, catq_kv_cache c, bf16* ko, bf16* vo) {
+  const int lph = g.d >> 3;
+  const int s = blockIdx.y;
+  const KvSeq q = kv_seq(g, s);
+  const int64_t per = (int64_t)g.n_kv * lph;
+  const int64_t total = (int64_t)q.n * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / per;
+    const int hs = (int)(i - t * per), h = hs / lph, sub = hs % lph;
+    const int64_t pos = q.ctx + t;
+    float k[8], v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) k[j] = v[j] = 0.f;
+    const int page = pos >= 0 && pos < kv_capacity(g)
+                         ? g.table[(int64_t)s * g.max_pages + (pos >> g.ps_log2)] : -1;
+    if (page >= 0 && page < g.n_pages) {
+      const int tok = (int)(pos & ((1 << g.ps_log2) - 1));
+      const int64_t si = kv_scale_index(g, page, h, tok);
+      if (ko) {
+        const uint2 w = *reinterpret_cast<const uint2*>(c.k + kv_code_base(g, page, h, tok) + sub * 8);
+        const float sc = c.k_scale[si];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          k[j] = code_of(w.x, j) * sc;
+          k[4 + j] = code_of(w.y, j) * sc;
+        }
+      }
+      if (vo) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(c.v + kv_code_base(g, page, h, tok & ~3) + sub * 32);
+        const u32x4 a0 = p[0], a1 = p[1];
+        const float sc = c.v_scale[si];
+        const int sh = 8 * (tok & 3);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[j] = code_of(a0[j] >> sh, 0) * sc;
+          v[4 + j] = code_of(a1[j] >> sh, 0) * sc;
+        }
+      }
+    }
+    const int64_t o = ((q.row0 + t) * g.n_kv + h) * g.d + sub * 8;
+    if (ko) store8<bf16>(ko + o, k);
+    if (vo) store8<bf16>(vo + o, v);
+  }
+}
+
+template <int LPH>
+catq_status launch_append(AppendArgs a, int64_t blocks, double bytes, hipStream_t stream) {
+  constexpr int TP = 256 / LPH;
+  auto go = [&](auto np) {
+    constexpr int NP = decltype(np)::value;
+    CATQ_TRACED(stream, "kv_append_kernel", 0.0, bytes, a.g.n_tokens, a.g.n_q + 2 * a.g.n_kv, a.g.d,
+                hipLaunchKernelGGL((kv_append_kernel<LPH, NP>), dim3((unsigned)blocks), dim3(256), 0,
+                                   stream, a));
+  };
+  using std::integral_constant;
+  const int passes = ((1 << a.w_log2) + TP - 1) / TP;   // a power of two
+  switch (passes) {
+    case 1: go(integral_constant<int, 1>{}); break;
+    case 2: go(integral_constant<int, 2>{}); break;
+    case 4: go(integral_constant<int, 4>{}); break;
+    // a window has at most 128 tokens: more passes only where fewer fit one
+    case 8:
+      if constexpr (TP <= 16) go(integral_constant<int, 8>{});
+      break;
+    default:
+      if constexpr (TP <= 8) go(integral_constant<int, 16>{});
+      break;
+  }
+  CATQ_CHECK_LAUNCH("kv append");
+  return CATQ_OK;
+}
+
+}  // namespace
+}  // namespace catq
+
+using namespace catq;
+
+extern "C" catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                          const catq_kv_batch* batch, const catq_kv_prep* prep,
+                                          const void* qkv, void* q_out, hipStream_t stream) {
+  clear_error();
+  CATQ_TRY(kv_check(d, cache, batch));
+  CATQ_REQUIRE(prep, CATQ_ERR_NULL, "prep must not be NULL");
+  CATQ_REQUIRE(prep->rot_dim >= 0 && prep->rot_dim <= d->head_dim && prep->rot_dim % 16 == 0,
+               CATQ_ERR_SHAPE, "rot_dim must be a multiple of 16, at most head_dim");
+  CATQ_REQUIRE(prep->rot_dim == 0 || prep->inv_freq, CATQ_ERR_NULL, "inv_freq must not be NULL");
+  CATQ_REQUIRE((prep->interleaved | prep->qk_norm | prep->act_quant) >> 1 == 0, CATQ_ERR_VALUE,
+               "interleaved, qk_norm and act_quant must be 0 or 1");
+  CATQ_REQUIRE(prep->eps >= 0.0f, CATQ_ERR_VALUE, "eps must be >= 0");
+  if (batch->n_seqs == 0 || batch->n_tokens == 0 || batch->max_new == 0) return CATQ_OK;
+  CATQ_REQUIRE(qkv && q_out, CATQ_ERR_NULL, "qkv and q_out must not be NULL");
+  CATQ_REQUIRE(aligned16(qkv) && aligned16(q_out) && aligned16(prep->q_weight) &&
+                   aligned16(prep->k_weight) && aligned16(prep->inv_freq),
+               CATQ_ERR_ALIGN, "misaligned");
+  AppendArgs a{};
+  a.g = kv_geom(d, batch);
+  a.c = *cache;
+  a.inv_freq = prep->inv_freq;
+  a.q_w = static_cast<const bf16*>(prep->q_weight);
+  a.k_w = static_cast<const bf16*>(prep->k_weight);
+  a.qkv = static_cast<const bf16*>(qkv);
+  a.q_out = static_cast<bf16*>(q_out);
+  a.rot = prep->rot_dim;
+  a.inter = prep->interleaved;
+  a.qk_norm = prep->qk_norm;
+  a.act_quant = prep->act_quant;
+  a.rope_scale = prep->rope_scale;
+  a.eps = prep->eps;
+  const int lph = d->head_dim / 8, tp = 256 / lph;
+  // a window lies in one page
+  const int w = d->scale_block > tp ? d->scale_block : (tp < d->page_size ? tp : d->page_size);
+  a.w_log2 = __builtin_ctz((unsigned)w);
+  a.win = (batch->max_new + w - 2) / w + 1;
+  a.q_parts = (d->n_q + tp - 1) / tp;
+  const int64_t max_blocks = INT32_MAX;
+  CATQ_REQUIRE((int64_t)a.win * batch->n_seqs <= max_blocks / (2 * d->n_kv), CATQ_ERR_SHAPE,
+               "too many sequences and new tokens for one launch");
+  a.kv_blocks = (int64_t)a.win * batch->n_seqs * d->n_kv * 2;
+  const int64_t blocks = a.kv_blocks + batch->n_tokens * a.q_parts;
+  CATQ_REQUIRE(blocks <= max_blocks, CATQ_ERR_SHAPE, "too many tokens for one launch");
+  const double e = (double)batch->n_tokens * d->head_dim;
+  const double bytes = e * (4.0 * d->n_q + 6.0 * d->n_kv);
+  switch (lph) {
+    case 8: return launch_append<8>(a, blocks, bytes, stream);
+    case 16: return launch_append<16>(a, blocks, bytes, stream);
+    default: return launch_append<32>(a, blocks, bytes, stream);
+  }
+}
+
+extern "C" catq_status catq_aux_kv_read(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                        const catq_kv_batch* batch, void* k_out, void* v_out,
+                                        hipStream_t stream) {
+  clear_error();
+  CATQ_TRY(kv_check(d, cache, batch));
+  CATQ_REQUIRE(aligned16(k_out) && aligned16(v_out), CATQ_ERR_ALIGN, "misaligned");
+  if (batch->n_seqs == 0 || batch->n_tokens == 0 || batch->max_new == 0) return CATQ_OK;
+  CATQ_REQUIRE(k_out || v_out, CATQ_ERR_NULL, "one of k_out and v_out must be given");
+  const int64_t per_seq = (int64_t)batch->max_new * d->n_kv * (d->head_dim / 8);
+  const unsigned gx = (unsigned)((per_seq + 255) / 256 < (1 << 20) ? (per_seq + 255) / 256 : (1 << 20));
+  const double bytes = (double)batch->n_tokens * d->n_kv * d->head_dim * ((k_out ? 3.0 : 0) + (v_out ? 3.0 : 0));
+  CATQ_TRACED(stream, "kv_read_kernel", 0.0, bytes, batch->n_tokens, d->n_kv, d->head_dim,
+              hipLaunchKernelGGL(kv_read_kernel, dim3(gx, (unsigned)batch->n_seqs), dim3(256), 0, stream,
+                                 kv_geom(d, batch), *cache, (bf16*)k_out, (bf16*)v_out));
+  CATQ_CHECK_LAUNCH("kv read");
+  return CATQ_OK;
+}
