@@ -51,6 +51,7 @@ struct PaArgs {
   float* part_ml;    // [span][token][head][2]
   int32_t G;         // query heads per kv head
   int32_t row_tiles; // of a sequence and kv head
+  int32_t tile_rows; // of a workgroup
   int32_t spans;
   int32_t span;      // tokens of a span: a multiple of 128
   int32_t limit;     // no position from here on is read: the pages' and the spans' end
@@ -372,9 +373,281 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
   }
 }
 
+// ------------------------------------------------------------------ many rows
+//
+// A workgroup takes 128 rows, 32 per wave, and 64-token tiles of the span: the four waves
+// convert a tile's codes once, into LDS as fp16 operands, and each forms S^T = K Q^T and
+// O^T = V^T P^T of its rows with v_mfma_f32_32x32x16_f16. As above a lane holds one query
+// (column lane % 32), its scores of a 32-token block are the tokens 8 qd + 4 h + e (h = lane / 32)
+// in register 4 qd + e, and those are, in order, the contraction slots of the second
+// product when the v operand takes the four-token words 4 T + h and 4 T + 2 + h of each 16 tokens.
+//   s_k [slice ks][h][token ^ 2 ks]: values 16 ks + 8 h .. + 7 of the token, 16 bytes
+//   s_v [T][h][d ^ (d / 16 % 4)]: the eight tokens of those two words at value d, 16 bytes
+// (reads and writes of 16 lanes in 16 different 16-byte banks). LDS is double-buffered, one
+// barrier per tile; the codes of the next tile are loaded while this one is multiplied.
+// A tile's v scale is in lv (log2, NaN outside its range, -inf on a page that does not
+// exist) and rv (its reciprocal, always finite, so that a masked token adds 0).
+constexpr int kRows = 128, kTile = 64;
+
+template <int D, bool PER_TOKEN>
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PaArgs a) {
+  constexpr int KS = D / 16;            // contraction slices of the scores
+  constexpr int DB = D / 32;            // output blocks
+  constexpr int KP = D / 64;            // 16-byte pieces of k per thread
+  __shared__ __align__(16) u32x4 s_k[2][KS * 2 * kTile];
+  __shared__ __align__(16) u32x4 s_v[2][8 * D];
+  __shared__ __align__(16) float s_ks[2][kTile], s_lv[2][kTile], s_rv[2][kTile];
+  const KvGeom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hh = lane >> 5, l32 = lane & 31;
+  unsigned b = blockIdx.x;
+  const int h = b % g.n_kv;
+  b /= g.n_kv;
+  const int rt = a.row_tiles - 1 - (int)(b % a.row_tiles);   // the longest rows first
+  const int sp = b / a.row_tiles, s = blockIdx.y;
+  const KvSeq q = kv_seq(g, s);
+  const int rows = q.n * a.G, r0 = rt * kRows;
+  if (r0 >= rows) return;
+  const int vmax = visible(a, q, (min(r0 + kRows, rows) - 1) / a.G);
+  const int c0 = sp * a.span;
+  if (sp > 0 && c0 >= vmax) return;      // the join knows which spans are there
+  const int c1 = min(vmax, c0 + a.span);
+  // this wave's rows
+  const int w0 = r0 + 32 * wave;
+  const bool has_rows = w0 < rows;
+  const int row = min(w0 + l32, rows - 1), qi = row / a.G, hq = h * a.G + (row - qi * a.G);
+  const int vis = visible(a, q, qi);
+  const int wmin = visible(a, q, min(w0, rows - 1) / a.G);
+  const int wmax = has_rows ? visible(a, q, min(w0 + 31, rows - 1) / a.G) : 0;
+
+  // queries: fp16 of q over the power of two at its row's largest magnitude
+  f16x8 qf[KS];
+  float qc;
+  {
+    const bf16* qp = a.Q + ((q.row0 + qi) * g.n_q + hq) * D + 8 * hh;
+    float m = 0.f;
+    u32x4 raw[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      raw[k] = *reinterpret_cast<const u32x4*>(qp + 16 * k);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m = fmaxf(m, fmaxf(fabsf(bf16_lo(raw[k][j])), fabsf(bf16_hi(raw[k][j]))));
+    }
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const int e = min(max((int)(__float_as_uint(m) >> 23) - 127, -100), 126);
+    const float down = __uint_as_float((unsigned)(127 - e) << 23);
+    qc = __uint_as_float((unsigned)(127 + e) << 23) * a.c;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        qf[k][2 * j] = (f16)(bf16_lo(raw[k][j]) * down);
+        qf[k][2 * j + 1] = (f16)(bf16_hi(raw[k][j]) * down);
+      }
+  }
+
+  const int32_t* table = g.table + (int64_t)s * g.max_pages;
+  const int ps_mask = (1 << g.ps_log2) - 1;
+  auto page_of = [&](int tok) {
+    const int pg = tok < vmax ? table[tok >> g.ps_log2] : -1;
+    return pg < 0 || pg >= g.n_pages ? -1 : pg;
+  };
+  // staging: k piece p = tid + 256 i is values 16 (p % KS) .. + 15 of token p / KS; v: thread tid takes
+  // values 4 d4 .. + 3 of word rows 4 T + vh and 4 T + 2 + vh
+  constexpr int VT = D / 4;                // threads per (T, vh)
+  constexpr bool kAllV = VT * 8 >= 256;    // (head_dim 64: half of the threads)
+  const int d4 = tid % VT, vt = tid / VT, vT = (vt >> 1) & 3, vh = vt & 1;
+  const bool v_mine = kAllV || vt < 8;
+  int pk[KP], pv, pp;
+  auto pages = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KP; ++i) pk[i] = page_of(t0 + (tid + 256 * i) / KS);
+    pv = page_of(t0 + 16 * vT);
+    pp = page_of(t0 + lane);
+  };
+  u32x4 kc[KP], vc[2];
+  float ksr, vsr;
+  bool none;
+  auto fetch = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      const int p = tid + 256 * i, tok = t0 + p / KS;
+      kc[i] = *reinterpret_cast<const u32x4*>(
+          a.K + kv_code_base(g, max(pk[i], 0), h, tok & ps_mask) + 16 * (p % KS));
+    }
+    const int8_t* vp = a.V + kv_code_base(g, max(pv, 0), h, (t0 + 16 * vT + 4 * vh) & ps_mask) + 16 * d4;
+    vc[0] = *reinterpret_cast<const u32x4*>(vp);
+    vc[1] = *reinterpret_cast<const u32x4*>(vp + 8 * D);
+    const int64_t si = kv_scale_index(g, max(pp, 0), h, (t0 + lane) & ps_mask);
+    ksr = a.KS[si];
+    vsr = a.VS[si];
+    none = pp < 0;
+  };
+  auto stage = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      const int p = tid + 256 * i, tok = p / KS, ks = p % KS;
+      s_k[buf][(2 * ks) * kTile + (tok ^ (2 * ks & 15))] = __builtin_bit_cast(u32x4, codes8(kc[i][0], kc[i][1]));
+      s_k[buf][(2 * ks + 1) * kTile + (tok ^ (2 * ks & 15))] = __builtin_bit_cast(u32x4, codes8(kc[i][2], kc[i][3]));
+    }
+    if (v_mine) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int d = 4 * d4 + e;
+        s_v[buf][(2 * vT + vh) * D + (d ^ ((d >> 4) & 3))] =
+            __builtin_bit_cast(u32x4, codes8(vc[0][e], vc[1][e]));
+      }
+    }
+    if (wave == 0) {
+      const bool tiny = vsr < kTinyScale, fine = vsr <= kHugeScale && !tiny;
+      s_ks[buf][lane] = none ? 0.f : ksr;
+      s_lv[buf][lane] = none ? -INFINITY : fine ? __builtin_amdgcn_logf(vsr) : tiny ? -60.f : __builtin_nanf("");
+      s_rv[buf][lane] = none || !(fine || tiny) ? 1.f : __builtin_amdgcn_rcpf(fine ? vsr : kTinyScale);
+    }
+  };
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  // m: the running maximum, 0 until the row has seen a token; limit: what a score may exceed it by
+  float m = 0.f, l = 0.f, limit = -INFINITY;
+
+  if (c0 < c1) {
+    pages(c0);
+    fetch(c0);
+    pages(c0 + kTile);
+  }
+  int buf = 0;
+  for (int t0 = c0; t0 < c1; t0 += kTile, buf ^= 1) {
+    stage(buf);
+    __syncthreads();
+    if (t0 + kTile < c1) {
+      fetch(t0 + kTile);
+      pages(t0 + 2 * kTile);
+    }
+    if (t0 >= wmax) continue;   // (the wave still stages what the others need)
+    f32x16 x[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[u][i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        x[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+            __builtin_bit_cast(f16x8, s_k[buf][(2 * k + hh) * kTile + ((32 * u + l32) ^ (2 * k & 15))]), qf[k], x[u],
+            0, 0, 0);
+    }
+    // scores over the running maximum: one scale per 16 tokens (two groups of four registers), or per token
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int qd = 0; qd < 4; ++qd) {
+        if constexpr (PER_TOKEN) {
+          const f32x4 k4 = *reinterpret_cast<const f32x4*>(&s_ks[buf][32 * u + 8 * qd + 4 * hh]);
+          const f32x4 l4 = *reinterpret_cast<const f32x4*>(&s_lv[buf][32 * u + 8 * qd + 4 * hh]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[u][4 * qd + e] = fmaf(x[u][4 * qd + e], k4[e] * qc, l4[e] - m);
+        } else {
+          const float kq = s_ks[buf][32 * u + 16 * (qd >> 1)] * qc, lm = s_lv[buf][32 * u + 16 * (qd >> 1)] - m;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[u][4 * qd + e] = fmaf(x[u][4 * qd + e], kq, lm);
+        }
+      }
+    if (t0 + kTile > wmin) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (t0 + 32 * u + 8 * (i >> 2) + 4 * hh + (i & 3) >= vis) x[u][i] = -INFINITY;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[u][i]);
+    if (__any(mx > limit)) {
+      // raise the maximum to the largest score of the row (of both halves' tokens); the first
+      // one seen sets it, also below 0
+      const float rm = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const bool first = limit != kRaise, any = rm > -INFINITY;
+      const float up = first ? (any ? rm : 0.f) : fmaxf(rm, 0.f);
+      const float f = first ? 1.0f : exp2_fast(-up);
+      limit = any ? kRaise : limit;
+      m += up;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[u][i] -= up;
+    }
+    f16x8 p[2][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int qd = 0; qd < 4; ++qd) {
+        float w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e] = exp2_fast(x[u][4 * qd + e]);
+          p[u][qd >> 1][4 * (qd & 1) + e] = (f16)w[e];
+        }
+        if constexpr (PER_TOKEN) {
+          const f32x4 r4 = *reinterpret_cast<const f32x4*>(&s_rv[buf][32 * u + 8 * qd + 4 * hh]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) l = fmaf(w[e], r4[e], l);
+        } else {
+          l = fmaf((w[0] + w[1]) + (w[2] + w[3]), s_rv[buf][32 * u + 16 * (qd >> 1)], l);
+        }
+      }
+#pragma unroll
+    for (int T = 0; T < 4; ++T)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const int dd = 32 * d + l32;
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+            __builtin_bit_cast(f16x8, s_v[buf][(2 * T + hh) * D + (dd ^ ((dd >> 4) & 3))]), p[T >> 1][T & 1], o[d], 0,
+            0, 0);
+      }
+  }
+  if (!has_rows || w0 + l32 >= rows) return;
+  const float L = l + __shfl_xor(l, 32, 64);
+  const int64_t at = (q.row0 + qi) * g.n_q + hq;
+  // register 4 qd + e of block d: value 32 d + 8 qd + 4 hh + e
+  if (a.spans > 1) {
+    const int64_t pa = (int64_t)sp * g.n_tokens * g.n_q + at;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int qd = 0; qd < 4; ++qd)
+        *reinterpret_cast<f32x4*>(a.part_o + pa * D + 32 * d + 8 * qd + 4 * hh) =
+            f32x4{o[d][4 * qd], o[d][4 * qd + 1], o[d][4 * qd + 2], o[d][4 * qd + 3]};
+    if (hh == 0) {
+      a.part_ml[2 * pa] = limit == kRaise || L != 0.f ? m : kNone;
+      a.part_ml[2 * pa + 1] = L;
+    }
+    return;
+  }
+  const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);   // (a NaN stays)
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int qd = 0; qd < 4; ++qd)
+      *reinterpret_cast<uint2*>(a.O + at * D + 32 * d + 8 * qd + 4 * hh) =
+          make_uint2(pack_bf16x2(o[d][4 * qd] * inv, o[d][4 * qd + 1] * inv),
+                     pack_bf16x2(o[d][4 * qd + 2] * inv, o[d][4 * qd + 3] * inv));
+  if (a.lse && hh == 0)
+    a.lse[at] = L == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+}
+
 // The spans of a row joined: one workgroup per (token, query head); its D / 4 lanes of
 // four values each take every (1024 / D)-th span.
-template <int D, int NR>
+template <int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
   constexpr int LN = D / 4, GR = 256 / LN;
   __shared__ __align__(16) float s_o[GR][D];
@@ -390,8 +663,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
   const KvSeq q = kv_seq(g, lo);
   if (t < q.row0 || t >= q.row0 + q.n) return;
   const int i = (int)(t - q.row0);
-  const int r0 = (i * a.G + hq % a.G) / (16 * NR) * (16 * NR);
-  const int vmax = visible(a, q, (min(r0 + 16 * NR, q.n * a.G) - 1) / a.G);
+  const int r0 = (i * a.G + hq % a.G) / a.tile_rows * a.tile_rows;
+  const int vmax = visible(a, q, (min(r0 + a.tile_rows, q.n * a.G) - 1) / a.G);
   const int live = max((vmax + a.span - 1) / a.span, 1);
   const int gr = threadIdx.x / LN, d4 = (threadIdx.x % LN) * 4;
   const int64_t at = t * g.n_q + hq, step = g.n_tokens * g.n_q;
@@ -437,19 +710,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
     a.lse[at] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
 }
 
-// How a call is split: rows per workgroup and spans of the context.
+// How a call is split: rows per workgroup (16 or 32: the waves split the context; 128: the
+// waves split the rows) and spans of the context.
 struct Plan {
-  int nr, row_tiles, spans, span;
+  int tile_rows, row_tiles, spans, span;
 };
 Plan plan(const catq_kv_desc* d, const catq_kv_batch* b) {
   const int64_t rows = (int64_t)b->max_new * (d->n_q / d->n_kv);
   Plan p;
-  p.nr = rows <= 16 ? 1 : rows <= 32 || d->head_dim == 256 ? 2 : 4;
-  p.row_tiles = (int)((rows + 16 * p.nr - 1) / (16 * p.nr));
-  // spans so that the chip has 2048 workgroups where the context allows, none under 256 tokens
+  p.tile_rows = rows <= 16 ? 16 : rows <= 32 || d->head_dim == 256 ? 32 : kRows;
+  p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
+  // spans so that the chip has enough workgroups where the context allows, none under 256 tokens
   const int64_t base = (int64_t)p.row_tiles * d->n_kv * b->n_seqs;
   const int64_t len = b->max_len > 0 ? b->max_len : 1;
-  const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(base, 1));
+  const int64_t want = std::max<int64_t>(1, (p.tile_rows == kRows ? 512 : 2048) / std::max<int64_t>(base, 1));
   int64_t span = (len + want - 1) / want;
   span = std::max<int64_t>(256, (span + 127) / 128 * 128);
   p.spans = (int)((len + span - 1) / span);
@@ -458,29 +732,25 @@ Plan plan(const catq_kv_desc* d, const catq_kv_batch* b) {
 }
 
 template <int D>
-catq_status launch_paged(const PaArgs& a, const Plan& p, bool per_token, double flops, double bytes,
-                         hipStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)p.row_tiles * p.spans * a.g.n_kv), (unsigned)a.g.n_seqs);
-  auto with = [&](auto nr, auto pt) {
-    constexpr int NR = decltype(nr)::value;
-    constexpr bool PT = decltype(pt)::value;
-    CATQ_TRACED(stream, "paged_attn_kernel", flops, bytes, a.g.n_tokens, a.g.n_q, D,
-                hipLaunchKernelGGL((paged_attn_kernel<D, NR, PT>), grid, dim3(256), 0, stream, a));
-    if (p.spans > 1)
-      CATQ_TRACED(stream, "paged_join_kernel", 0.0,
-                  (double)a.g.n_tokens * a.g.n_q * D * (4.0 * p.spans + 2.0), a.g.n_tokens, a.g.n_q, D,
-                  hipLaunchKernelGGL((paged_join_kernel<D, NR>), dim3((unsigned)(a.g.n_tokens * a.g.n_q)),
-                                     dim3(256), 0, stream, a));
+catq_status launch_paged(const PaArgs& a, bool per_token, double flops, double bytes, hipStream_t stream) {
+  const dim3 grid((unsigned)((int64_t)a.row_tiles * a.spans * a.g.n_kv), (unsigned)a.g.n_seqs);
+  static char tag[64];
+  trace_tag(tag, sizeof tag, "paged_attn<%d rows, head_dim %d>", a.tile_rows, D);
+  auto go = [&](auto kernel) {
+    CATQ_TRACED(stream, tag, flops, bytes, a.g.n_tokens, a.g.n_q, D,
+                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a));
   };
-  auto rows = [&](auto nr) {
-    if (per_token) with(nr, std::true_type{});
-    else with(nr, std::false_type{});
-  };
-  using std::integral_constant;
-  if (p.nr == 1) rows(integral_constant<int, 1>{});
-  else if (p.nr == 2) rows(integral_constant<int, 2>{});
-  else if constexpr (D <= 128) rows(integral_constant<int, 4>{});
+  if (a.tile_rows == 16) per_token ? go(paged_attn_kernel<D, 1, true>) : go(paged_attn_kernel<D, 1, false>);
+  else if (a.tile_rows == 32) per_token ? go(paged_attn_kernel<D, 2, true>) : go(paged_attn_kernel<D, 2, false>);
+  else if constexpr (D <= 128) per_token ? go(paged_tile_kernel<D, true>) : go(paged_tile_kernel<D, false>);
   CATQ_CHECK_LAUNCH("paged attention");
+  if (a.spans > 1) {
+    CATQ_TRACED(stream, "paged_join_kernel", 0.0, (double)a.g.n_tokens * a.g.n_q * D * (4.0 * a.spans + 2.0),
+                a.g.n_tokens, a.g.n_q, D,
+                hipLaunchKernelGGL((paged_join_kernel<D>), dim3((unsigned)(a.g.n_tokens * a.g.n_q)), dim3(256), 0,
+                                   stream, a));
+    CATQ_CHECK_LAUNCH("paged attention join");
+  }
   return CATQ_OK;
 }
 
@@ -538,6 +808,7 @@ extern "C" catq_status catq_aux_paged_attention(const catq_kv_desc* d, const cat
   }
   a.G = d->n_q / d->n_kv;
   a.row_tiles = p.row_tiles;
+  a.tile_rows = p.tile_rows;
   a.spans = p.spans;
   a.span = p.span;
   a.limit = (int32_t)std::min<int64_t>((int64_t)d->max_pages * d->page_size, (int64_t)p.spans * p.span);
@@ -546,8 +817,8 @@ extern "C" catq_status catq_aux_paged_attention(const catq_kv_desc* d, const cat
   const double flops = 4.0 * (double)batch->n_tokens * batch->max_len * d->n_q * d->head_dim;
   const double bytes = 2.0 * (double)batch->n_seqs * batch->max_len * d->n_kv * d->head_dim;
   switch (d->head_dim) {
-    case 64: return launch_paged<64>(a, p, per_token, flops, bytes, stream);
-    case 128: return launch_paged<128>(a, p, per_token, flops, bytes, stream);
-    default: return launch_paged<256>(a, p, per_token, flops, bytes, stream);
+    case 64: return launch_paged<64>(a, per_token, flops, bytes, stream);
+    case 128: return launch_paged<128>(a, per_token, flops, bytes, stream);
+    default: return launch_paged<256>(a, per_token, flops, bytes, stream);
   }
 }
