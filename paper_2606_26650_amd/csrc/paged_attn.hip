@@ -387,16 +387,18 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
 // barrier per tile; the codes of the next tile are loaded while this one is multiplied.
 // A tile's v scale is in lv (log2, NaN outside its range, -inf on a page that does not
 // exist) and rv (its reciprocal, always finite, so that a masked token adds 0).
-constexpr int kRows = 128, kTile = 64;
+constexpr int kTile = 64;
 
-template <int D, bool PER_TOKEN>
-__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PaArgs a) {
+template <int D, int NW, bool PER_TOKEN>
+__global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
   constexpr int KS = D / 16;            // contraction slices of the scores
   constexpr int DB = D / 32;            // output blocks
-  constexpr int KP = D / 64;            // 16-byte pieces of k per thread
+  constexpr int NT = NW * 64, kRows = NW * 32;
+  constexpr int KP = (4 * D + NT - 1) / NT;   // 16-byte pieces of k per thread
   __shared__ __align__(16) u32x4 s_k[2][KS * 2 * kTile];
   __shared__ __align__(16) u32x4 s_v[2][8 * D];
   __shared__ __align__(16) float s_ks[2][kTile], s_lv[2][kTile], s_rv[2][kTile];
+  __shared__ int s_tiny[2];
   const KvGeom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, l32 = lane & 31;
@@ -452,48 +454,85 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PaArgs a) {
     const int pg = tok < vmax ? table[tok >> g.ps_log2] : -1;
     return pg < 0 || pg >= g.n_pages ? -1 : pg;
   };
-  // staging: k piece p = tid + 256 i is values 16 (p % KS) .. + 15 of token p / KS; v: thread tid takes
-  // values 4 d4 .. + 3 of word rows 4 T + vh and 4 T + 2 + vh
-  constexpr int VT = D / 4;                // threads per (T, vh)
-  constexpr bool kAllV = VT * 8 >= 256;    // (head_dim 64: half of the threads)
-  const int d4 = tid % VT, vt = tid / VT, vT = (vt >> 1) & 3, vh = vt & 1;
-  const bool v_mine = kAllV || vt < 8;
-  int pk[KP], pv, pp;
-  auto pages = [&](int t0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < KP; ++i) pk[i] = page_of(t0 + (tid + 256 * i) / KS);
-    pv = page_of(t0 + 16 * vT);
-    pp = page_of(t0 + lane);
-  };
-  u32x4 kc[KP], vc[2];
+  // staging: k piece p = tid + NT i is values 16 (p % KS) .. + 15 of token p / KS; v: thread tid
+  // takes values VD dv .. + VD - 1 of word rows 4 T + vh and 4 T + 2 + vh
+  constexpr int VD = 8 * D >= NT * 4 ? 4 : 8 * D >= NT * 2 ? 2 : 1;
+  constexpr int VT = D / VD;               // threads per (T, vh)
+  constexpr bool kAllK = 4 * D >= NT, kAllV = VT * 8 >= NT;   // (else some threads have none)
+  const int dv = VD * (tid % VT), vt = tid / VT, vT = (vt >> 1) & 3, vh = vt & 1;
+  const bool k_mine = kAllK || tid < 4 * D, v_mine = kAllV || vt < 8;
+  static_assert(VT * 8 <= NT, "one v task per thread");
+  typedef __attribute__((ext_vector_type(VD))) unsigned int vwords;
+  u32x4 kc[KP];
+  vwords vc[2];
   float ksr, vsr;
   bool none;
+  // a page's bytes in either code array, and its scales, with the head's place in them
+  const unsigned page_codes = (unsigned)(g.n_kv << g.ps_log2) * D, head_codes = (unsigned)(h << g.ps_log2) * D;
+  const unsigned page_scales = (unsigned)g.n_kv << (g.ps_log2 - g.bt_log2),
+                 head_scales = (unsigned)h << (g.ps_log2 - g.bt_log2);
+  // places inside the tile
+  const int kt = (tid % (4 * D)) / KS, vtok = 16 * vT + 4 * vh;
+  const unsigned koff = 16 * (tid % KS), voff = 4 * dv;
+  // the next tile's pages: one for all of it where a page holds whole tiles, one per lane's part
+  // of it (each k piece, its v words, token `lane`) elsewhere
+  const bool one_page = g.ps_log2 >= 6;
+  int pk[KP], pv, pp;
+  auto pages = [&](int t0) __attribute__((always_inline)) {
+    if (one_page) {
+      pp = page_of(__builtin_amdgcn_readfirstlane(t0));
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < KP; ++i) pk[i] = page_of(t0 + kt + i * (NT / KS));
+    pv = page_of(t0 + vtok);
+    pp = page_of(t0 + lane);
+  };
   auto fetch = [&](int t0) __attribute__((always_inline)) {
+    if (one_page) {
+      const int pg = __builtin_amdgcn_readfirstlane(pp), t = t0 & ps_mask;
+      const uint64_t base = (uint64_t)(unsigned)max(pg, 0) * page_codes + (head_codes + (unsigned)t * D);
+      const int8_t *kb = a.K + base, *vb = a.V + base;
+#pragma unroll
+      for (int i = 0; i < KP; ++i)
+        kc[i] = *reinterpret_cast<const u32x4*>(kb + ((unsigned)(kt + i * (NT / KS)) * D + koff));
+      vc[0] = *reinterpret_cast<const vwords*>(vb + ((unsigned)vtok * D + voff));
+      vc[1] = *reinterpret_cast<const vwords*>(vb + ((unsigned)(vtok + 8) * D + voff));
+      const uint64_t sb = (uint64_t)(unsigned)max(pg, 0) * page_scales + (head_scales + ((unsigned)t >> g.bt_log2));
+      ksr = a.KS[sb + ((unsigned)lane >> g.bt_log2)];
+      vsr = a.VS[sb + ((unsigned)lane >> g.bt_log2)];
+      none = pg < 0;
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < KP; ++i) {
-      const int p = tid + 256 * i, tok = t0 + p / KS;
-      kc[i] = *reinterpret_cast<const u32x4*>(
-          a.K + kv_code_base(g, max(pk[i], 0), h, tok & ps_mask) + 16 * (p % KS));
+      const unsigned off = head_codes + (unsigned)((t0 + kt + i * (NT / KS)) & ps_mask) * D + koff;
+      kc[i] = *reinterpret_cast<const u32x4*>(a.K + ((uint64_t)(unsigned)max(pk[i], 0) * page_codes + off));
     }
-    const int8_t* vp = a.V + kv_code_base(g, max(pv, 0), h, (t0 + 16 * vT + 4 * vh) & ps_mask) + 16 * d4;
-    vc[0] = *reinterpret_cast<const u32x4*>(vp);
-    vc[1] = *reinterpret_cast<const u32x4*>(vp + 8 * D);
-    const int64_t si = kv_scale_index(g, max(pp, 0), h, (t0 + lane) & ps_mask);
+    const unsigned off = head_codes + (unsigned)((t0 + vtok) & ps_mask) * D + voff;
+    const int8_t* vp = a.V + ((uint64_t)(unsigned)max(pv, 0) * page_codes + off);
+    vc[0] = *reinterpret_cast<const vwords*>(vp);
+    vc[1] = *reinterpret_cast<const vwords*>(vp + 8 * D);
+    const uint64_t si = (uint64_t)(unsigned)max(pp, 0) * page_scales +
+                        (head_scales + ((unsigned)((t0 + lane) & ps_mask) >> g.bt_log2));
     ksr = a.KS[si];
     vsr = a.VS[si];
     none = pp < 0;
   };
   auto stage = [&](int buf) __attribute__((always_inline)) {
+    if (k_mine) {
 #pragma unroll
-    for (int i = 0; i < KP; ++i) {
-      const int p = tid + 256 * i, tok = p / KS, ks = p % KS;
-      s_k[buf][(2 * ks) * kTile + (tok ^ (2 * ks & 15))] = __builtin_bit_cast(u32x4, codes8(kc[i][0], kc[i][1]));
-      s_k[buf][(2 * ks + 1) * kTile + (tok ^ (2 * ks & 15))] = __builtin_bit_cast(u32x4, codes8(kc[i][2], kc[i][3]));
+      for (int i = 0; i < KP; ++i) {
+        const int tok = kt + i * (NT / KS), ks = tid % KS;
+        s_k[buf][(2 * ks) * kTile + (tok ^ (2 * ks & 15))] = __builtin_bit_cast(u32x4, codes8(kc[i][0], kc[i][1]));
+        s_k[buf][(2 * ks + 1) * kTile + (tok ^ (2 * ks & 15))] =
+            __builtin_bit_cast(u32x4, codes8(kc[i][2], kc[i][3]));
+      }
     }
     if (v_mine) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int d = 4 * d4 + e;
+      for (int e = 0; e < VD; ++e) {
+        const int d = dv + e;
         s_v[buf][(2 * vT + vh) * D + (d ^ ((d >> 4) & 3))] =
             __builtin_bit_cast(u32x4, codes8(vc[0][e], vc[1][e]));
       }
@@ -503,6 +542,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PaArgs a) {
       s_ks[buf][lane] = none ? 0.f : ksr;
       s_lv[buf][lane] = none ? -INFINITY : fine ? __builtin_amdgcn_logf(vsr) : tiny ? -60.f : __builtin_nanf("");
       s_rv[buf][lane] = none || !(fine || tiny) ? 1.f : __builtin_amdgcn_rcpf(fine ? vsr : kTinyScale);
+      s_tiny[buf] = __any(tiny && !none);
     }
   };
 
@@ -530,15 +570,16 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PaArgs a) {
     if (t0 >= wmax) continue;   // (the wave still stages what the others need)
     f32x16 x[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[u][i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
         x[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
             __builtin_bit_cast(f16x8, s_k[buf][(2 * k + hh) * kTile + ((32 * u + l32) ^ (2 * k & 15))]), qf[k], x[u],
             0, 0, 0);
-    }
     // scores over the running maximum: one scale per 16 tokens (two groups of four registers), or per token
     float mx = -INFINITY;
 #pragma unroll
@@ -605,6 +646,13 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PaArgs a) {
           l = fmaf((w[0] + w[1]) + (w[2] + w[3]), s_rv[buf][32 * u + 16 * (qd >> 1)], l);
         }
       }
+    if (__builtin_amdgcn_readfirstlane(s_tiny[buf])) {   // some scales count as 0: their tokens' terms are 0
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (s_lv[buf][32 * u + 8 * (i >> 2) + 4 * hh + (i & 3)] == -60.f) p[u][i >> 3][i & 7] = (f16)0.f;
+    }
 #pragma unroll
     for (int T = 0; T < 4; ++T)
 #pragma unroll
@@ -715,15 +763,18 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
 struct Plan {
   int tile_rows, row_tiles, spans, span;
 };
+#ifndef PA_T
+#define PA_T 128
+#endif
 Plan plan(const catq_kv_desc* d, const catq_kv_batch* b) {
   const int64_t rows = (int64_t)b->max_new * (d->n_q / d->n_kv);
   Plan p;
-  p.tile_rows = rows <= 16 ? 16 : rows <= 32 || d->head_dim == 256 ? 32 : kRows;
+  p.tile_rows = rows <= 16 ? 16 : rows <= 32 || d->head_dim == 256 ? 32 : rows <= PA_T ? 128 : 256;
   p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
   // spans so that the chip has enough workgroups where the context allows, none under 256 tokens
   const int64_t base = (int64_t)p.row_tiles * d->n_kv * b->n_seqs;
   const int64_t len = b->max_len > 0 ? b->max_len : 1;
-  const int64_t want = std::max<int64_t>(1, (p.tile_rows == kRows ? 512 : 2048) / std::max<int64_t>(base, 1));
+  const int64_t want = std::max<int64_t>(1, (p.tile_rows >= 128 ? 512 : 2048) / std::max<int64_t>(base, 1));
   int64_t span = (len + want - 1) / want;
   span = std::max<int64_t>(256, (span + 127) / 128 * 128);
   p.spans = (int)((len + span - 1) / span);
@@ -738,11 +789,14 @@ catq_status launch_paged(const PaArgs& a, bool per_token, double flops, double b
   trace_tag(tag, sizeof tag, "paged_attn<%d rows, head_dim %d>", a.tile_rows, D);
   auto go = [&](auto kernel) {
     CATQ_TRACED(stream, tag, flops, bytes, a.g.n_tokens, a.g.n_q, D,
-                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a));
+                hipLaunchKernelGGL(kernel, grid, dim3(a.tile_rows == 256 ? 512 : 256), 0, stream, a));
   };
   if (a.tile_rows == 16) per_token ? go(paged_attn_kernel<D, 1, true>) : go(paged_attn_kernel<D, 1, false>);
   else if (a.tile_rows == 32) per_token ? go(paged_attn_kernel<D, 2, true>) : go(paged_attn_kernel<D, 2, false>);
-  else if constexpr (D <= 128) per_token ? go(paged_tile_kernel<D, true>) : go(paged_tile_kernel<D, false>);
+  else if constexpr (D <= 128) {
+    if (a.tile_rows == 128) per_token ? go(paged_tile_kernel<D, 4, true>) : go(paged_tile_kernel<D, 4, false>);
+    else per_token ? go(paged_tile_kernel<D, 8, true>) : go(paged_tile_kernel<D, 8, false>);
+  }
   CATQ_CHECK_LAUNCH("paged attention");
   if (a.spans > 1) {
     CATQ_TRACED(stream, "paged_join_kernel", 0.0, (double)a.g.n_tokens * a.g.n_q * D * (4.0 * a.spans + 2.0),

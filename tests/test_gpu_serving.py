@@ -593,6 +593,23 @@ def test_attention_scales_past_the_range(catq, bt, new):
         assert torch.equal(torch.isnan(lse[r0:r0 + n].cpu()), bad)
 
 
+@pytest.mark.parametrize("bt", [1, 32])
+@pytest.mark.parametrize("new", [1, 20, 300])
+def test_attention_tiny_scales_count_as_zero(catq, bt, new):
+    """Below 2^-60 a v scale is 0, whatever its codes are: the output is exactly 0, and so is it
+    where the others' tokens are far below it."""
+    sv = Serving(catq, [(40, new)], 2, 1, 128, 64, bt)
+    sv.vs[:] = 2.0 ** -61
+    sv.upload()
+    q = _rand(sv.g, new, 256)
+    ws = torch.empty(max(1, catq.catq_paged_attention_workspace_bytes(sv.desc, sv.batch)), dtype=torch.uint8,
+                     device="cuda")
+    o = torch.empty((new, 256), dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty((new, 2), device="cuda")
+    catq.catq_aux_paged_attention(sv.desc, sv.cache, sv.batch, q.cuda(), o, ws, lse=lse)
+    assert (o == 0).all() and torch.isfinite(lse).all()
+
+
 def test_attention_masked_contents_do_not_count(catq):
     """NaN and infinite scales at positions that a row does not see, and on a page that is
     not the sequence's, change nothing; one that a row sees reaches that row."""
