@@ -381,13 +381,13 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
 // (column lane % 32), its scores of a 32-token block are the tokens 8 qd + 4 h + e (h = lane / 32)
 // in register 4 qd + e, and those are, in order, the contraction slots of the second
 // product when the v operand takes the four-token words 4 T + h and 4 T + 2 + h of each 16 tokens.
-//   s_k [slice ks][h][token ^ 2 ks]: values 16 ks + 8 h .. + 7 of the token, 16 bytes
-//   s_v [T][h][d ^ (d / 16 % 4)]: the eight tokens of those two words at value d, 16 bytes
-// (reads and writes of 16 lanes in 16 different 16-byte banks). LDS is double-buffered, one
+//   s_k [slice ks][h][token], 65 tokens apart: values 16 ks + 8 h .. + 7 of the token, 16 bytes
+//   s_v [T][h][d]: the eight tokens of those two words at value d, 16 bytes
+// (16 lanes read, and write k, in 16 different 16-byte banks; one lane address for all reads). LDS is double-buffered, one
 // barrier per tile; the codes of the next tile are loaded while this one is multiplied.
 // A tile's v scale is in lv (log2, NaN outside its range, -inf on a page that does not
 // exist) and rv (its reciprocal, always finite, so that a masked token adds 0).
-constexpr int kTile = 64;
+constexpr int kTile = 64, kPitch = kTile + 1;
 
 template <int D, int NW, bool PER_TOKEN>
 __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
   constexpr int DB = D / 32;            // output blocks
   constexpr int NT = NW * 64, kRows = NW * 32;
   constexpr int KP = (4 * D + NT - 1) / NT;   // 16-byte pieces of k per thread
-  __shared__ __align__(16) u32x4 s_k[2][KS * 2 * kTile];
+  __shared__ __align__(16) u32x4 s_k[2][KS * 2 * kPitch];
   __shared__ __align__(16) u32x4 s_v[2][8 * D];
   __shared__ __align__(16) float s_ks[2][kTile], s_lv[2][kTile], s_rv[2][kTile];
   __shared__ int s_tiny[2];
@@ -524,8 +524,8 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
 #pragma unroll
       for (int i = 0; i < KP; ++i) {
         const int tok = kt + i * (NT / KS), ks = tid % KS;
-        s_k[buf][(2 * ks) * kTile + (tok ^ (2 * ks & 15))] = __builtin_bit_cast(u32x4, codes8(kc[i][0], kc[i][1]));
-        s_k[buf][(2 * ks + 1) * kTile + (tok ^ (2 * ks & 15))] =
+        s_k[buf][(2 * ks) * kPitch + tok] = __builtin_bit_cast(u32x4, codes8(kc[i][0], kc[i][1]));
+        s_k[buf][(2 * ks + 1) * kPitch + tok] =
             __builtin_bit_cast(u32x4, codes8(kc[i][2], kc[i][3]));
       }
     }
@@ -533,7 +533,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
 #pragma unroll
       for (int e = 0; e < VD; ++e) {
         const int d = dv + e;
-        s_v[buf][(2 * vT + vh) * D + (d ^ ((d >> 4) & 3))] =
+        s_v[buf][(2 * vT + vh) * D + d] =
             __builtin_bit_cast(u32x4, codes8(vc[0][e], vc[1][e]));
       }
     }
@@ -578,7 +578,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
         x[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-            __builtin_bit_cast(f16x8, s_k[buf][(2 * k + hh) * kTile + ((32 * u + l32) ^ (2 * k & 15))]), qf[k], x[u],
+            __builtin_bit_cast(f16x8, s_k[buf][(2 * k + hh) * kPitch + 32 * u + l32]), qf[k], x[u],
             0, 0, 0);
     // scores over the running maximum: one scale per 16 tokens (two groups of four registers), or per token
     float mx = -INFINITY;
@@ -656,12 +656,10 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
 #pragma unroll
     for (int T = 0; T < 4; ++T)
 #pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const int dd = 32 * d + l32;
+      for (int d = 0; d < DB; ++d)
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-            __builtin_bit_cast(f16x8, s_v[buf][(2 * T + hh) * D + (dd ^ ((dd >> 4) & 3))]), p[T >> 1][T & 1], o[d], 0,
+            __builtin_bit_cast(f16x8, s_v[buf][(2 * T + hh) * D + 32 * d + l32]), p[T >> 1][T & 1], o[d], 0,
             0, 0);
-      }
   }
   if (!has_rows || w0 + l32 >= rows) return;
   const float L = l + __shfl_xor(l, 32, 64);
