@@ -691,14 +691,19 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
     a.lse[at] = L == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
 }
 
-// The spans of a row joined: one workgroup per (token, query head); its D / 4 lanes of
-// four values each take every (1024 / D)-th span.
+// The spans of a row joined: one workgroup per (token, query head). Every span's weight
+// first, 2^(its maximum - the row's), all of them at once into LDS; then the weighted sum of the
+// partial outputs, D / 4 lanes of four values by 1024 / D spans, loads that wait for nothing.
+// (With a running maximum over the spans instead, 256 spans took 12 us.)
+constexpr int kMaxSpans = 512;
+
 template <int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
   constexpr int LN = D / 4, GR = 256 / LN;
   __shared__ __align__(16) float s_o[GR][D];
-  __shared__ float s_m[GR], s_l[GR];
+  __shared__ float s_w[kMaxSpans], s_red[4];
   const KvGeom& g = a.g;
+  const int tid = threadIdx.x, wave = tid >> 6;
   const int64_t t = blockIdx.x / g.n_q;
   const int hq = blockIdx.x % g.n_q;
   int lo = 0, hi = g.n_seqs;
@@ -712,40 +717,47 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
   const int r0 = (i * a.G + hq % a.G) / a.tile_rows * a.tile_rows;
   const int vmax = visible(a, q, (min(r0 + a.tile_rows, q.n * a.G) - 1) / a.G);
   const int live = max((vmax + a.span - 1) / a.span, 1);
-  const int gr = threadIdx.x / LN, d4 = (threadIdx.x % LN) * 4;
   const int64_t at = t * g.n_q + hq, step = g.n_tokens * g.n_q;
-  float m = kNone, l = 0.f;
+  float M = kNone;
+  for (int sp = tid; sp < live; sp += 256) {
+    const float pm = a.part_ml[2 * (sp * step + at)];
+    s_w[sp] = pm;
+    M = fmaxf(M, pm);
+  }
+  M = wave_max(M);
+  if ((tid & 63) == 0) s_red[wave] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+  __syncthreads();
+  float L = 0.f;
+  for (int sp = tid; sp < live; sp += 256) {
+    const float w = exp2_fast(s_w[sp] - M);
+    L = fmaf(a.part_ml[2 * (sp * step + at) + 1], w, L);
+    s_w[sp] = w;
+  }
+  L = wave_sum(L);
+  if ((tid & 63) == 0) s_red[wave] = L;
+  __syncthreads();
+  L = (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]);
+  const int gr = tid / LN, d4 = (tid % LN) * 4;
+  const float* po = a.part_o + at * D + d4;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int sp = gr; sp < live; sp += GR) {
-    const int64_t pa = sp * step + at;
-    const float pm = a.part_ml[2 * pa], pl = a.part_ml[2 * pa + 1];
-    const f32x4 po = *reinterpret_cast<const f32x4*>(a.part_o + pa * D + d4);
-    const float mn = fmaxf(m, pm);
-    const float f = exp2_fast(m - mn), fp = exp2_fast(pm - mn);
-    m = mn;
-    l = l * f + pl * fp;
+    const float w = s_w[sp];
+    const f32x4 v = *reinterpret_cast<const f32x4*>(po + sp * step * D);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = y[j] * f + po[j] * fp;
+    for (int j = 0; j < 4; ++j) y[j] = fmaf(v[j], w, y[j]);
   }
   *reinterpret_cast<f32x4*>(&s_o[gr][d4]) = y;
-  if (d4 == 0) {
-    s_m[gr] = m;
-    s_l[gr] = l;
-  }
   __syncthreads();
   if (gr != 0) return;
-  float M = s_m[0];
+  f32x4 z = y;
 #pragma unroll
-  for (int k = 1; k < GR; ++k) M = fmaxf(M, s_m[k]);
-  float L = 0.f;
-  f32x4 z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int k = 0; k < GR; ++k) {
-    const float f = exp2_fast(s_m[k] - M);
-    L += s_l[k] * f;
+  for (int k = 1; k < GR; ++k) {
     const f32x4 w = *reinterpret_cast<const f32x4*>(&s_o[k][d4]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) z[j] += w[j] * f;
+    for (int j = 0; j < 4; ++j) z[j] += w[j];
   }
   const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
   uint2 out;
@@ -769,10 +781,13 @@ Plan plan(const catq_kv_desc* d, const catq_kv_batch* b) {
   Plan p;
   p.tile_rows = rows <= 16 ? 16 : rows <= 32 || d->head_dim == 256 ? 32 : rows <= PA_T ? 128 : 256;
   p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
-  // spans so that the chip has enough workgroups where the context allows, none under 256 tokens
+  // Spans so that the chip has 512 workgroups where the context allows (131072 tokens of one sequence:
+  // 58 us; 62 with 1024, 67 with 2048), none under 256 tokens (1000 tokens of one sequence: 9.9 us; 12.4
+  // where none is under 512), and one up to 512, where the join costs more than it gives (300 tokens:
+  // 7.8 us, 10.2 in two spans).
   const int64_t base = (int64_t)p.row_tiles * d->n_kv * b->n_seqs;
   const int64_t len = b->max_len > 0 ? b->max_len : 1;
-  const int64_t want = std::max<int64_t>(1, (p.tile_rows >= 128 ? 512 : 2048) / std::max<int64_t>(base, 1));
+  const int64_t want = len <= 512 ? 1 : std::max<int64_t>(1, 512 / std::max<int64_t>(base, 1));
   int64_t span = (len + want - 1) / want;
   span = std::max<int64_t>(256, (span + 127) / 128 * 128);
   p.spans = (int)((len + span - 1) / span);
