@@ -2,21 +2,20 @@
 // the rotation on the way, and values back out.
 //
 // Append.  One launch, two kinds of workgroups:
-//  * q: a workgroup takes one token and as many query heads as 256 threads cover
-//    at eight values each; its rotation angles are formed once in LDS.
+//  * q: a workgroup takes one token and as many query heads as 256 threads cover at
+//    sixteen values each; the rotation angles are formed once in LDS.
 //  * k and v: a workgroup takes a window of W tokens of one kv head of K or V, W the
-//    larger of a scale block and what 256 threads cover (16 tokens of 128), so it
+//    larger of a scale block and what 256 threads cover (32 tokens of 128), so it
 //    owns whole scale blocks and whole four-token words of the v layout: no other
 //    workgroup reads or writes them.  It keeps the window's values in registers
-//    (eight per thread and pass of 256 threads), reduces their magnitudes to the blocks'
+//    (sixteen per thread and pass of 256 threads), reduces their magnitudes to the blocks'
 //    scales through LDS, and writes codes (v through a transposed LDS tile, so that
 //    four tokens make one word).  Where a block holds older tokens and its scale
 //    grows, their codes are read, rescaled and written with the new ones.
-// A few new tokens cost a launch and two memory latencies; many are HBM bound.
-//
-// Angles are taken in float64: position * inv_freq reaches 1e6 radians, where a
-// product in fp32 is off by 0.06; the fraction of a turn is then exact to 1e-10 and
-// its sine and cosine are fp32.
+// A few new tokens cost a launch and three memory latencies in a row (lengths, page, scale; 64
+// single tokens: 7.5 us). Many: 9400 tokens of 32 + 8 + 8 heads of 128 take 55 us, 3.9 TB/s; the rotation and
+// the quantizer's vector instructions are what the rest is (72 us with one value in
+// each lane's pairs and the angles in float64).
 #include <type_traits>
 
 #include "kv_common.h"
@@ -87,114 +86,154 @@ struct AppendArgs {
   int32_t q_parts;      // workgroups per token for the query heads
 };
 
-// cos and sin of `n` consecutive positions from pos0, [token][rot/2], times the scale
-__device__ __forceinline__ void angles(const AppendArgs& a, int64_t pos0, int n, float2* cs, int nt) {
+// cos and sin of `n` positions from pos0 on, times the scale, at cs[t][rot/2]: by one wave, a
+// lane per frequency. The turns are pos * inv_freq / 2 pi with the factor in two floats (of
+// 48 bits together, from float64), less the whole ones inside an fma: off by 2^-25 of a turn
+// below position 2^24, in five operations where float64 takes a hundred cycles; float64 beyond.
+__device__ __forceinline__ void angles(const AppendArgs& a, int64_t pos0, int n, float2* cs) {
   const int half = a.rot >> 1;
-  for (int i = threadIdx.x; i < n * half; i += nt) {
-    const int t = i / half, f = i - t * half;
-    // in half turns: the fraction is what counts
-    const double turn = (double)(pos0 + t) * (double)a.inv_freq[f] * 0.31830988618379067154;
-    const float r = (float)(turn - 2.0 * rint(turn * 0.5));
-    float s, c;
-    sincospif(r, &s, &c);
-    cs[i] = make_float2(c * a.rope_scale, s * a.rope_scale);
+  for (int f = threadIdx.x & 63; f < half; f += 64) {
+    const double turn = (double)a.inv_freq[f] * 0.15915494309189533577;
+    const float hi = (float)turn, lo = (float)(turn - (double)hi);
+    for (int t = 0; t < n; ++t) {
+      const int64_t pos = pos0 + t;
+      float r;
+      if (pos < (1 << 24)) {
+        const float x = (float)pos, whole = rintf(x * hi);
+        r = fmaf(x, lo, fmaf(x, hi, -whole));
+      } else {
+        const double p = (double)pos * turn;
+        r = (float)(p - rint(p));
+      }
+      float s, c;
+      sincospif(2.0f * r, &s, &c);
+      cs[t * half + f] = make_float2(c * a.rope_scale, s * a.rope_scale);
+    }
   }
 }
 
-// Eight values of a head held by lane `sub` of LPH: norm (with its gain) and rotation.
+// A head is held by LPH lanes of sixteen values each, in two runs of eight at `a` and `b`: a lane
+// has both sides of its pairs, value 8 sub + j and the one rot/2 further on (or, interleaved and
+// where nothing rotates, sixteen neighbours), and needs the angles 8 sub .. + 7.
+struct HeadPart {
+  int a, b;
+  bool turn;
+};
+__device__ __forceinline__ HeadPart head_part(const AppendArgs& a, int sub) {
+  const int lanes = a.rot >> 4;
+  if (a.inter) return {16 * sub, 16 * sub + 8, sub < lanes};
+  if (sub < lanes) return {8 * sub, (a.rot >> 1) + 8 * sub, true};
+  return {16 * sub, 16 * sub + 8, false};
+}
+__device__ __forceinline__ void load16(const bf16* p, HeadPart h, float (&v)[16]) {
+  float x[8], y[8];
+  load8<bf16>(p + h.a, x);
+  load8<bf16>(p + h.b, y);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] = x[j];
+    v[8 + j] = y[j];
+  }
+}
+__device__ __forceinline__ unsigned int mag16(const float (&v)[16]) {
+  unsigned int m = 0u;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) m = max(m, mag_bits(v[j]));
+  return m;
+}
+
+// norm (with its gain) and rotation
 template <int LPH>
-__device__ __forceinline__ void prep_head(const AppendArgs& a, float (&v)[8], int sub, const bf16* w,
+__device__ __forceinline__ void prep_head(const AppendArgs& a, float (&v)[16], int sub, HeadPart h, const bf16* w,
                                           const float2* cs) {
-  constexpr int D = LPH * 8;
+  constexpr int D = LPH * 16;
   if (a.qk_norm) {
     float ss = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fmaf(v[j], v[j], ss);
+    for (int j = 0; j < 16; ++j) ss = fmaf(v[j], v[j], ss);
 #pragma unroll
     for (int m = LPH >> 1; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, 64);
     const float r = 1.0f / sqrtf(ss / (float)D + a.eps);
     if (w) {
-      float g[8];
-      load8<bf16>(w + sub * 8, g);
+      float g[16];
+      load16(w, h, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = v[j] * r * g[j];
+      for (int j = 0; j < 16; ++j) v[j] = v[j] * r * g[j];
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= r;
+      for (int j = 0; j < 16; ++j) v[j] *= r;
     }
   }
-  if (a.rot == 0) return;
-  const int lanes = a.rot >> 3;   // lanes that rotate
-  if (a.inter) {
-    if (sub < lanes) {
+  if (!h.turn) return;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 t = cs[sub * 4 + j];
-        const float x = v[2 * j], y = v[2 * j + 1];
-        v[2 * j] = x * t.x - y * t.y;
-        v[2 * j + 1] = y * t.x + x * t.y;
-      }
-    }
-    return;
-  }
-  const int hl = lanes >> 1;      // lanes of the first half
-  const int lane = threadIdx.x & 63, base = lane - sub;
-  const int other = sub < hl ? sub + hl : sub < lanes ? sub - hl : sub;
-  float p[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) p[j] = __shfl(v[j], base + other, 64);
-  if (sub < lanes) {
-    const int f0 = (sub < hl ? sub : other) * 8;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float2 t = cs[f0 + j];
-      v[j] = sub < hl ? v[j] * t.x - p[j] * t.y : v[j] * t.x + p[j] * t.y;
+  for (int j = 0; j < 8; ++j) {
+    const float2 t = cs[8 * sub + j];
+    if (a.inter) {
+      const float p = v[2 * j], q = v[2 * j + 1];
+      v[2 * j] = p * t.x - q * t.y;
+      v[2 * j + 1] = q * t.x + p * t.y;
+    } else {
+      const float p = v[j], q = v[8 + j];
+      v[j] = p * t.x - q * t.y;
+      v[8 + j] = q * t.x + p * t.y;
     }
   }
 }
 
+// One token and as many heads as fit the workgroup. (Four tokens a workgroup were slower, 62 us
+// against 55 for the prompts above.)
 template <int LPH>
-__device__ __forceinline__ void append_q(const AppendArgs& a, int64_t block, float2* cs, int* s_seq) {
-  constexpr int D = LPH * 8, HP = 256 / LPH;   // heads per workgroup
+__device__ __forceinline__ void append_q(const AppendArgs& a, int64_t block, float2* cs, int64_t* s_pos) {
+  constexpr int D = LPH * 16, HP = 256 / LPH;   // heads per workgroup
   const int64_t t = block / a.q_parts;
   const int part = (int)(block % a.q_parts);
-  // the token's sequence: the last one that starts at or before it (empty ones
-  // before it start there too)
+  const int sub = threadIdx.x & (LPH - 1), h = part * HP + threadIdx.x / LPH;
+  const bool live = h < a.g.n_q;
+  const HeadPart hp = head_part(a, sub);
+  float v[16];
+  if (live)
+    load16(a.qkv + t * (a.g.n_q + 2 * (int64_t)a.g.n_kv) * D + (int64_t)h * D, hp, v);
+  else
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = 0.f;
+  // the token's sequence: the last one that starts at or before it (empty ones before it start
+  // there too)
   if (threadIdx.x == 0) {
     int lo = 0, hi = a.g.n_seqs;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (a.g.cu[mid] <= t) lo = mid; else hi = mid;
     }
-    *s_seq = lo;
+    const KvSeq q = kv_seq(a.g, lo);
+    // (a row of no sequence)
+    *s_pos = t < q.row0 || t >= q.row0 + q.n ? INT64_MIN : q.ctx + (t - q.row0);
   }
   __syncthreads();
-  const KvSeq q = kv_seq(a.g, *s_seq);
-  if (t < q.row0 || t >= q.row0 + q.n) return;   // a row of no sequence
-  const int64_t pos = q.ctx + (t - q.row0);
-  angles(a, pos, 1, cs, 256);
+  const int64_t pos = *s_pos;
+  if (pos == INT64_MIN) return;
+  if (threadIdx.x < 64) angles(a, pos, 1, cs);
   __syncthreads();
-  const int sub = threadIdx.x & (LPH - 1), h = part * HP + threadIdx.x / LPH;
-  const bool live = h < a.g.n_q;
-  float v[8];
-  if (live)
-    load8<bf16>(a.qkv + t * (a.g.n_q + 2 * (int64_t)a.g.n_kv) * D + (int64_t)h * D + sub * 8, v);
-  else
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.f;
-  prep_head<LPH>(a, v, sub, a.q_w, cs);
+  prep_head<LPH>(a, v, sub, hp, a.q_w, cs);
   if (a.act_quant) {
-    unsigned int m = 0u;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, mag_bits(v[j]));
+    unsigned int m = mag16(v);
 #pragma unroll
     for (int k = LPH >> 1; k >= 1; k >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, k, 64));
     const float s = quant8_scale(m);
-    const Quant8 quant(s);
+    quant8_n(v, s);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = quant(v[j]) * s;
+    for (int j = 0; j < 16; ++j) v[j] *= s;
   }
-  if (live) store8<bf16>(a.q_out + (t * a.g.n_q + h) * D + sub * 8, v);
+  if (live) {
+    bf16* o = a.q_out + (t * a.g.n_q + h) * D;
+    float x[8], y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = v[j];
+      y[j] = v[8 + j];
+    }
+    store8<bf16>(o + hp.a, x);
+    store8<bf16>(o + hp.b, y);
+  }
 }
 
 // byte b of a word as a signed code
@@ -207,7 +246,7 @@ template <int LPH, int NP>
 __device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, float2* cs,
                                           unsigned int* s_mag, float* s_scale, float* s_ratio,
                                           unsigned char* s_tile) {
-  constexpr int D = LPH * 8, TP = 256 / LPH;
+  constexpr int D = LPH * 16, TP = 256 / LPH;
   const KvGeom& g = a.g;
   const int is_v = (int)(block & 1);
   block >>= 1;
@@ -221,8 +260,6 @@ __device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, fl
   const int64_t first = ((begin >> a.w_log2) + wi) << a.w_log2;
   const int64_t end = min((int64_t)q.ctx + q.n, kv_capacity(g));
   if (first >= end || begin >= end) return;
-  const int page = g.table[(int64_t)s * g.max_pages + (first >> g.ps_log2)];
-  if (page < 0 || page >= g.n_pages) return;
   const int tok0 = (int)(first & ((1 << g.ps_log2) - 1));   // of the page
   const int lo = (int)max(begin - first, (int64_t)0), hi = (int)min(end - first, (int64_t)W);
   const int bt = 1 << g.bt_log2;
@@ -232,33 +269,38 @@ __device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, fl
 
   const int sub = threadIdx.x & (LPH - 1), tl = threadIdx.x / LPH;
   const int64_t ld = (g.n_q + 2 * (int64_t)g.n_kv) * D;
-  const bf16* src = a.qkv + (int64_t)(g.n_q + (is_v ? g.n_kv : 0) + h) * D + sub * 8;
-  float v[NP][8];
+  const HeadPart hp = is_v ? HeadPart{16 * sub, 16 * sub + 8, false} : head_part(a, sub);
+  const bf16* src = a.qkv + (int64_t)(g.n_q + (is_v ? g.n_kv : 0) + h) * D;
+  // (the values are on their way while the page is looked up)
+  const int page = g.table[(int64_t)s * g.max_pages + (first >> g.ps_log2)];
+  float v[NP][16];
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int t = p * TP + tl;
     if (t >= lo && t < hi) {
-      load8<bf16>(src + (q.row0 + (first + t - q.ctx)) * ld, v[p]);
+      load16(src + (q.row0 + (first + t - q.ctx)) * ld, hp, v[p]);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[p][j] = 0.f;
+      for (int j = 0; j < 16; ++j) v[p][j] = 0.f;
     }
   }
+  if (page < 0 || page >= g.n_pages) return;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int t = p * TP + tl;
     if (!is_v) {
       if (p > 0) __syncthreads();   // the table of the pass before is read
-      if (p * TP < hi && (p + 1) * TP > lo) angles(a, first + p * TP, TP, cs, 256);
+      // of the pass's new tokens, a quarter by each wave
+      const int ta = max(lo - p * TP, 0), n = min(hi - p * TP, TP) - ta, w = threadIdx.x >> 6;
+      const int w0 = n * w >> 2, w1 = n * (w + 1) >> 2;
+      if (n > 0) angles(a, first + p * TP + ta + w0, w1 - w0, cs + (ta + w0) * (a.rot >> 1));
       __syncthreads();
-      prep_head<LPH>(a, v[p], sub, a.k_w, cs + tl * (a.rot >> 1));
+      prep_head<LPH>(a, v[p], sub, hp, a.k_w, cs + tl * (a.rot >> 1));
       if (t < lo || t >= hi)        // (a norm turns zeros into zeros, an angle may be anything)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[p][j] = 0.f;
+        for (int j = 0; j < 16; ++j) v[p][j] = 0.f;
     }
-    unsigned int m = 0u;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, mag_bits(v[p][j]));
+    unsigned int m = mag16(v[p]);
 #pragma unroll
     for (int k = LPH >> 1; k >= 1; k >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, k, 64));
     if (sub == 0 && t < W) s_mag[t] = m;
@@ -291,35 +333,34 @@ __device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, fl
   for (int p = 0; p < NP; ++p) {
     const int t = p * TP + tl;
     if (t < wlo || t >= hi) continue;
-    unsigned int c0, c1;
     if (t < lo) {   // an older token of the block whose scale grew
       const float r = s_ratio[0];
-      float o[8];
       if (is_v) {
-        const int8_t* vp = codes + cbase + (int64_t)(t >> 2) * (4 * D) + sub * 32 + (t & 3);
+        const int8_t* vp = codes + cbase + (int64_t)(t >> 2) * (4 * D) + 4 * hp.a + (t & 3);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = rintf((float)vp[4 * j] * r);
+        for (int j = 0; j < 16; ++j) v[p][j] = rintf((float)vp[4 * j] * r);
       } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(codes + cbase + (int64_t)t * D + sub * 8);
+        const int8_t* kp = codes + cbase + (int64_t)t * D;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          o[j] = rintf(code_of(w.x, j) * r);
-          o[4 + j] = rintf(code_of(w.y, j) * r);
+        for (int j = 0; j < 8; ++j) {
+          v[p][j] = rintf((float)kp[hp.a + j] * r);
+          v[p][8 + j] = rintf((float)kp[hp.b + j] * r);
         }
       }
-      c0 = pack_codes(o[0], o[1], o[2], o[3]);
-      c1 = pack_codes(o[4], o[5], o[6], o[7]);
     } else {
-      const Quant8 quant(s_scale[t >> g.bt_log2]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[p][j] = quant(v[p][j]);
-      c0 = pack_codes(v[p][0], v[p][1], v[p][2], v[p][3]);
-      c1 = pack_codes(v[p][4], v[p][5], v[p][6], v[p][7]);
+      quant8_n(v[p], s_scale[t >> g.bt_log2]);
     }
-    if (is_v)
-      *reinterpret_cast<uint2*>(s_tile + t * D + sub * 8) = make_uint2(c0, c1);
-    else
-      *reinterpret_cast<uint2*>(codes + cbase + (int64_t)t * D + sub * 8) = make_uint2(c0, c1);
+    const uint2 c0 = make_uint2(pack_codes(v[p][0], v[p][1], v[p][2], v[p][3]),
+                                pack_codes(v[p][4], v[p][5], v[p][6], v[p][7]));
+    const uint2 c1 = make_uint2(pack_codes(v[p][8], v[p][9], v[p][10], v[p][11]),
+                                pack_codes(v[p][12], v[p][13], v[p][14], v[p][15]));
+    if (is_v) {
+      *reinterpret_cast<uint2*>(s_tile + t * D + hp.a) = c0;
+      *reinterpret_cast<uint2*>(s_tile + t * D + hp.b) = c1;
+    } else {
+      *reinterpret_cast<uint2*>(codes + cbase + (int64_t)t * D + hp.a) = c0;
+      *reinterpret_cast<uint2*>(codes + cbase + (int64_t)t * D + hp.b) = c1;
+    }
   }
   if (!is_v) return;
   __syncthreads();
@@ -342,18 +383,18 @@ __device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, fl
 
 template <int LPH, int NP>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
-  constexpr int D = LPH * 8, TP = 256 / LPH;
+  constexpr int D = LPH * 16, TP = 256 / LPH;
   __shared__ float2 cs[TP * D / 2];
   __shared__ unsigned int s_mag[TP * NP];
   __shared__ float s_scale[TP * NP];
   __shared__ float s_ratio[1];
-  __shared__ int s_seq;
+  __shared__ int64_t s_pos;
   __shared__ __align__(16) unsigned char s_tile[TP * NP * D];
   const int64_t b = blockIdx.x;
   if (b < a.kv_blocks)
     append_kv<LPH, NP>(a, b, cs, s_mag, s_scale, s_ratio, s_tile);
   else
-    append_q<LPH>(a, b - a.kv_blocks, cs, &s_seq);
+    append_q<LPH>(a, b - a.kv_blocks, cs, &s_pos);
 }
 
 // Eight values of one (token, head) per thread.  A v word holds four tokens: the
@@ -405,7 +446,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvGeom g, catq_kv_cache c,
 }
 
 template <int LPH>
-catq_status launch_append(AppendArgs a, int64_t blocks, double bytes, hipStream_t stream) {
+catq_status launch_append(const AppendArgs& a, int64_t blocks, double bytes, hipStream_t stream) {
   constexpr int TP = 256 / LPH;
   auto go = [&](auto np) {
     constexpr int NP = decltype(np)::value;
@@ -418,13 +459,14 @@ catq_status launch_append(AppendArgs a, int64_t blocks, double bytes, hipStream_
   switch (passes) {
     case 1: go(integral_constant<int, 1>{}); break;
     case 2: go(integral_constant<int, 2>{}); break;
-    case 4: go(integral_constant<int, 4>{}); break;
+    case 4:
+      if constexpr (TP <= 32) go(integral_constant<int, 4>{});
+      break;
     // a window has at most 128 tokens: more passes only where fewer fit one
     case 8:
       if constexpr (TP <= 16) go(integral_constant<int, 8>{});
       break;
     default:
-      if constexpr (TP <= 8) go(integral_constant<int, 16>{});
       break;
   }
   CATQ_CHECK_LAUNCH("kv append");
@@ -467,7 +509,7 @@ extern "C" catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_c
   a.act_quant = prep->act_quant;
   a.rope_scale = prep->rope_scale;
   a.eps = prep->eps;
-  const int lph = d->head_dim / 8, tp = 256 / lph;
+  const int lph = d->head_dim / 16, tp = 256 / lph;
   // a window lies in one page
   const int w = d->scale_block > tp ? d->scale_block : (tp < d->page_size ? tp : d->page_size);
   a.w_log2 = __builtin_ctz((unsigned)w);
@@ -482,9 +524,9 @@ extern "C" catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_c
   const double e = (double)batch->n_tokens * d->head_dim;
   const double bytes = e * (4.0 * d->n_q + 6.0 * d->n_kv);
   switch (lph) {
+    case 4: return launch_append<4>(a, blocks, bytes, stream);
     case 8: return launch_append<8>(a, blocks, bytes, stream);
-    case 16: return launch_append<16>(a, blocks, bytes, stream);
-    default: return launch_append<32>(a, blocks, bytes, stream);
+    default: return launch_append<16>(a, blocks, bytes, stream);
   }
 }
 

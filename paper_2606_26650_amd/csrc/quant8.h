@@ -14,23 +14,30 @@ __device__ __forceinline__ float quant8_scale(unsigned int mag) {
   return mag >= 0x7f800000u ? __builtin_nanf("") : __uint_as_float(mag) / 127.0f;
 }
 
-// rne(x / s) as a float.  The product with the reciprocal differs from the quotient
-// by less than 127 * 2^-22 = 3e-5, so the two round alike unless the product is that
-// near to a half: only then (and where 1/s overflows: the test fails for a NaN) is
-// the quotient formed.  |x| <= 127 s up to one rounding of a normal s, so only the
-// quotient by a subnormal s (1/s overflows) can need the clamp.  0 for s = 0 and for
-// a NaN scale.
-struct Quant8 {
-  float s, inv;
-  __device__ __forceinline__ explicit Quant8(float scale)
-      : s(scale > 0.f ? scale : 1.0f), inv(scale > 0.f ? 1.0f / scale : 0.0f) {}
-  __device__ __forceinline__ float operator()(float x) const {
-    const float t = x * inv;
-    float r = rintf(t);
-    if (!(fabsf(t - r) <= 0.4999f)) r = inv > 0.f ? fminf(fmaxf(rintf(x / s), -127.f), 127.f) : 0.f;
-    return r;
+// N values to rne(x / s), as floats.  The product with the reciprocal differs from the
+// quotient by less than 127 * 2^-22 = 3.03e-5, so the two round alike unless the product is that
+// near to a half: only where one of them is (and where 1/s overflows: the test fails for
+// a NaN) are the quotients formed.  |x| <= 127 s up to one rounding of a normal s, so only
+// the quotient by a subnormal s can need the clamp.  0 for s = 0 and for a NaN scale.
+template <int N>
+__device__ __forceinline__ void quant8_n(float (&x)[N], float scale) {
+  const bool some = scale > 0.f;
+  const float s = some ? scale : 1.0f, inv = some ? 1.0f / scale : 0.0f;
+  float r[N];
+  bool near = false;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float t = x[j] * inv;
+    r[j] = rintf(t);
+    near |= !(fabsf(t - r[j]) <= 0.49996f);
   }
-};
+  if (near) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) r[j] = some ? fminf(fmaxf(rintf(x[j] / s), -127.f), 127.f) : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) x[j] = r[j];
+}
 
 // Four codes (floats within +-127) as bytes, the first lowest.
 __device__ __forceinline__ unsigned int pack_codes(float a, float b, float c, float d) {
