@@ -298,30 +298,53 @@ def catq_aux_add(a, b, y, stream=None):
 # TypeError or ValueError here, before the library sees a pointer.  They run on the
 # device of their tensors and, without ``stream``, on that device's current stream.
 
-def _want(t, name, dtype, shape=None, device=None, strided=False):
-    if t.dtype != dtype if not isinstance(dtype, tuple) else t.dtype not in dtype:
+def _want(t, name, dtype, shape=None, device=None):
+    """t, a contiguous tensor of the dtype, shape and device (an index) asked for."""
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
-    if not t.is_contiguous() and not (strided and t.dim() == 2 and t.stride(1) == 1):
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
-    if device is None:
-        if not t.is_cuda:
+    if t.get_device() != device:
+        if device is None:
+            if t.is_cuda:
+                return t
             raise ValueError(f"{name}: must be on a GPU")
-    elif t.device != device:
-        raise ValueError(f"{name}: on {t.device}, expected {device}")
+        raise ValueError(f"{name}: on {t.device}, expected GPU {device}")
     return t
 
 
-_ACT = (torch.bfloat16, torch.float32)
+def _act(t, name):
+    """The catq dtype of an activation tensor (bf16 or fp32)."""
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected bfloat16 or float32")
+    return dt
+
+
+def _rows(t, name, shape, device):
+    """The row stride of a 2-d tensor whose rows are contiguous."""
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    if t.stride(1) != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, expected GPU {device}")
+    return t.stride(0) if shape[0] > 1 else shape[1]
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _run_on(device, stream, fn, name, *args):
-    if device.index == torch.cuda.current_device():
-        _lib.check(name, fn(*args, _stream(stream)))
+    if device == _current_device():
+        st = fn(*args, _stream(stream) if _raw_stream is None or stream is not None else _raw_stream(device))
     else:
         with torch.cuda.device(device):
-            _lib.check(name, fn(*args, _stream(stream)))
+            st = fn(*args, _stream(stream))
+    if st:
+        _lib.check(name, st)
 
 
 def _bytes(ws):
@@ -333,43 +356,50 @@ def catq_aux_rmsnorm_quant(x, q=None, scale=None, res=None, weight=None, sum=Non
     """h = x + res (into ``sum``), RMSNorm with gain ``weight``, and its 8-bit codes q
     with their scales [rows][n/group] (default: one per row), or their values y in
     bf16, or both."""
-    _want(x, "x", _ACT)
-    n, dev = x.shape[-1], x.device
+    xd = _act(x, "x")
+    _want(x, "x", x.dtype)
+    shape, dev = x.shape, x.get_device()
+    n = shape[-1]
     rows = x.numel() // n if n else 0
-    group = n if group is None else group
-    for t, name in ((res, "res"), (sum, "sum")):
-        if t is not None:
-            _want(t, name, _ACT, tuple(x.shape), dev)
-    if res is not None and sum is not None and res.dtype != sum.dtype:
-        raise TypeError(f"sum: dtype {sum.dtype}, expected {res.dtype}")
+    if group is None:
+        group = n
+    rd = BF16
+    if res is not None:
+        rd = _act(res, "res")
+        _want(res, "res", res.dtype, shape, dev)
+        if sum is not None:
+            _want(sum, "sum", res.dtype, shape, dev)
+    elif sum is not None:
+        raise ValueError("sum: needs res")
     if weight is not None:
         _want(weight, "weight", torch.bfloat16, (n,), dev)
     if y is not None:
-        _want(y, "y", torch.bfloat16, tuple(x.shape), dev)
+        _want(y, "y", torch.bfloat16, shape, dev)
     if q is not None:
-        _want(q, "q", torch.int8, tuple(x.shape), dev)
+        _want(q, "q", torch.int8, shape, dev)
     if scale is not None:
         _want(scale, "scale", torch.float32, None, dev)
         if group > 0 and scale.numel() != rows * (n // group):
             raise ValueError(f"scale: {scale.numel()} values, expected {rows * (n // group)}")
-    _run_on(dev, stream, lib.catq_aux_rmsnorm_quant, "catq_aux_rmsnorm_quant", _ptr(x), _dt(x), _ptr(res),
-            BF16 if res is None else _dt(res), _ptr(weight), rows, n, group, eps, _ptr(sum), _ptr(y), _ptr(q),
-            _ptr(scale))
+    _run_on(dev, stream, lib.catq_aux_rmsnorm_quant, "catq_aux_rmsnorm_quant", x.data_ptr(), xd, _ptr(res), rd,
+            _ptr(weight), rows, n, group, eps, _ptr(sum), _ptr(y), _ptr(q), _ptr(scale))
 
 
 def catq_aux_act_quant8(x, q, scale, group=None, stream=None):
     """The 8-bit codes of every group of ``group`` consecutive values of x's rows
     (default: the whole row) and their scales."""
-    _want(x, "x", _ACT)
-    n, dev = x.shape[-1], x.device
+    xd = _act(x, "x")
+    _want(x, "x", x.dtype)
+    n, dev = x.shape[-1], x.get_device()
     rows = x.numel() // n if n else 0
-    group = n if group is None else group
-    _want(q, "q", torch.int8, tuple(x.shape), dev)
+    if group is None:
+        group = n
+    _want(q, "q", torch.int8, x.shape, dev)
     _want(scale, "scale", torch.float32, None, dev)
     if group > 0 and scale.numel() != rows * (n // group):
         raise ValueError(f"scale: {scale.numel()} values, expected {rows * (n // group)}")
-    _run_on(dev, stream, lib.catq_aux_act_quant8, "catq_aux_act_quant8", _ptr(x), _dt(x), rows, n, group,
-            _ptr(q), _ptr(scale))
+    _run_on(dev, stream, lib.catq_aux_act_quant8, "catq_aux_act_quant8", x.data_ptr(), xd, rows, n, group,
+            q.data_ptr(), scale.data_ptr())
 
 
 def catq_ternary_linear_a8(q, x_scale, packed, alpha, Y, g=128, stream=None):
@@ -377,18 +407,21 @@ def catq_ternary_linear_a8(q, x_scale, packed, alpha, Y, g=128, stream=None):
     (rows may be strided), x_scale fp32 [M], packed uint8 [d_out][d_in/4], alpha
     fp32 [d_out][d_in/g], Y fp32 or bf16 [M][d_out] (rows may be strided)."""
     _want(packed, "packed", torch.uint8)
-    dev = packed.device
+    dev = packed.get_device()
     d_out, d_in = packed.shape[0], packed.shape[1] * 4
     M = q.shape[0]
-    _want(q, "q", torch.int8, (M, d_in), dev, strided=True)
-    _want(Y, "Y", _ACT, (M, d_out), dev, strided=True)
-    for t, name, n in ((x_scale, "x_scale", M), (alpha, "alpha", d_out * (d_in // g) if g > 0 else 0)):
-        _want(t, name, torch.float32, None, dev)
-        if g > 0 and t.numel() != n:
-            raise ValueError(f"{name}: {t.numel()} values, expected {n}")
-    _run_on(dev, stream, lib.catq_ternary_linear_a8, "catq_ternary_linear_a8", _ptr(q), M,
-            q.stride(0) if M > 1 else d_in, _ptr(x_scale), _ptr(packed), _ptr(alpha), d_out, d_in, g, _ptr(Y),
-            _dt(Y), Y.stride(0) if M > 1 else d_out)
+    if q.dtype is not torch.int8:
+        raise TypeError(f"q: dtype {q.dtype}, expected torch.int8")
+    yd = _act(Y, "Y")
+    ldq, ldy = _rows(q, "q", (M, d_in), dev), _rows(Y, "Y", (M, d_out), dev)
+    _want(x_scale, "x_scale", torch.float32, None, dev)
+    _want(alpha, "alpha", torch.float32, None, dev)
+    if x_scale.numel() != M:
+        raise ValueError(f"x_scale: {x_scale.numel()} values, expected {M}")
+    if g > 0 and alpha.numel() != d_out * (d_in // g):
+        raise ValueError(f"alpha: {alpha.numel()} values, expected {d_out * (d_in // g)}")
+    _run_on(dev, stream, lib.catq_ternary_linear_a8, "catq_ternary_linear_a8", q.data_ptr(), M, ldq,
+            x_scale.data_ptr(), packed.data_ptr(), alpha.data_ptr(), d_out, d_in, g, Y.data_ptr(), yd, ldy)
 
 
 def kv_desc(n_q, n_kv, head_dim, page_size, scale_block, n_pages, max_pages):
@@ -402,12 +435,13 @@ def kv_cache(desc, k, v, k_scale, v_scale):
     [n_pages][n_kv][page_size/scale_block].  The returned struct keeps them."""
     d = desc
     _want(k, "k", torch.int8, (d.n_pages, d.n_kv, d.page_size, d.head_dim))
-    _want(v, "v", torch.int8, (d.n_pages, d.n_kv, d.page_size // 4, d.head_dim, 4), k.device)
+    dev = k.get_device()
+    _want(v, "v", torch.int8, (d.n_pages, d.n_kv, d.page_size // 4, d.head_dim, 4), dev)
     blocks = (d.n_pages, d.n_kv, d.page_size // d.scale_block if d.scale_block > 0 else 0)
-    _want(k_scale, "k_scale", torch.float32, blocks, k.device)
-    _want(v_scale, "v_scale", torch.float32, blocks, k.device)
+    _want(k_scale, "k_scale", torch.float32, blocks, dev)
+    _want(v_scale, "v_scale", torch.float32, blocks, dev)
     c = KvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
-    c.tensors, c.device, c.geometry = (k, v, k_scale, v_scale), k.device, bytes(d)[:24]
+    c.tensors, c.device, c.geometry = (k, v, k_scale, v_scale), dev, bytes(d)[:24]
     return c
 
 
@@ -417,10 +451,11 @@ def kv_batch(desc, page_table, cu_new, ctx_len, n_tokens, max_new, max_len):
     device; their values may change between calls.  The returned struct keeps them."""
     n = ctx_len.shape[0]
     _want(page_table, "page_table", torch.int32, (n, desc.max_pages))
-    _want(cu_new, "cu_new", torch.int32, (n + 1,), page_table.device)
-    _want(ctx_len, "ctx_len", torch.int32, (n,), page_table.device)
+    dev = page_table.get_device()
+    _want(cu_new, "cu_new", torch.int32, (n + 1,), dev)
+    _want(ctx_len, "ctx_len", torch.int32, (n,), dev)
     b = KvBatch(page_table.data_ptr(), cu_new.data_ptr(), ctx_len.data_ptr(), n_tokens, n, max_new, max_len)
-    b.tensors, b.device = (page_table, cu_new, ctx_len), page_table.device
+    b.tensors, b.device, b.width = (page_table, cu_new, ctx_len), dev, desc.max_pages
     return b
 
 
@@ -429,7 +464,7 @@ def kv_prep(desc, inv_freq=None, rot_dim=0, interleaved=False, qk_norm=False, q_
     """What happens to q and k on the way to the cache (see catq_kv_prep in the
     header).  The returned struct keeps the tensors."""
     first = next((t for t in (inv_freq, q_weight, k_weight) if t is not None), None)
-    dev = None if first is None else first.device
+    dev = None if first is None else first.get_device()
     if inv_freq is not None:
         _want(inv_freq, "inv_freq", torch.float32, (rot_dim // 2,))
     for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
@@ -444,10 +479,10 @@ def kv_prep(desc, inv_freq=None, rot_dim=0, interleaved=False, qk_norm=False, q_
 def _kv_same(desc, cache, batch):
     dev = cache.device
     if batch.device != dev:
-        raise ValueError(f"batch: on {batch.device}, expected {dev}")
+        raise ValueError(f"batch: on GPU {batch.device}, expected {dev}")
     if bytes(desc)[:24] != cache.geometry:
         raise ValueError("the cache was made for another descriptor")
-    if batch.tensors[0].shape[1] != desc.max_pages:
+    if batch.width != desc.max_pages:
         raise ValueError("the batch's page table is not max_pages wide")
     return dev
 
@@ -457,7 +492,7 @@ def catq_aux_kv_append(desc, cache, batch, prep, qkv, q_out, stream=None):
     q into q_out [n_tokens][n_q head_dim], k and v into the cache."""
     dev, n, d = _kv_same(desc, cache, batch), batch.n_tokens, desc.head_dim
     if prep.device is not None and prep.device != dev:
-        raise ValueError(f"prep: on {prep.device}, expected {dev}")
+        raise ValueError(f"prep: on GPU {prep.device}, expected {dev}")
     _want(qkv, "qkv", torch.bfloat16, (n, (desc.n_q + 2 * desc.n_kv) * d), dev)
     _want(q_out, "q_out", torch.bfloat16, (n, desc.n_q * d), dev)
     _run_on(dev, stream, lib.catq_aux_kv_append, "catq_aux_kv_append", C.byref(desc), C.byref(cache),
@@ -486,8 +521,8 @@ def catq_aux_paged_attention(desc, cache, batch, q, o, workspace=None, scale=Non
     _want(o, "o", torch.bfloat16, shape, dev)
     if lse is not None:
         _want(lse, "lse", torch.float32, (batch.n_tokens, desc.n_q), dev)
-    if workspace is not None and workspace.device != dev:
-        raise ValueError(f"workspace: on {workspace.device}, expected {dev}")
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        raise ValueError(f"workspace: must be contiguous and on GPU {dev}")
     _run_on(dev, stream, lib.catq_aux_paged_attention, "catq_aux_paged_attention", C.byref(desc),
             C.byref(cache), C.byref(batch), _ptr(q), desc.head_dim ** -0.5 if scale is None else scale, _ptr(o),
             _ptr(lse), _ptr(workspace), _bytes(workspace))
