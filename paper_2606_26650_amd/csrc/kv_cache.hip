@@ -515,7 +515,7 @@ extern "C" catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_c
   a.w_log2 = __builtin_ctz((unsigned)w);
   a.win = (batch->max_new + w - 2) / w + 1;
   a.q_parts = (d->n_q + tp - 1) / tp;
-  const int64_t max_blocks = INT32_MAX;
+  const int64_t max_blocks = (1 << 24) - 1;   // (a launch has fewer than 2^32 threads along x)
   CATQ_REQUIRE((int64_t)a.win * batch->n_seqs <= max_blocks / (2 * d->n_kv), CATQ_ERR_SHAPE,
                "too many sequences and new tokens for one launch");
   a.kv_blocks = (int64_t)a.win * batch->n_seqs * d->n_kv * 2;

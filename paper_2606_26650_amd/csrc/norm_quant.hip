@@ -191,7 +191,8 @@ catq_status check_quant(int64_t rows, int64_t n, int64_t group) {
   CATQ_REQUIRE(n > 0 && group > 0 && n % group == 0 && group % 8 == 0, CATQ_ERR_SHAPE,
                "group must be a multiple of 8 dividing n");
   CATQ_REQUIRE(n <= 32768, CATQ_ERR_SHAPE, "n must be <= 32768");
-  CATQ_REQUIRE(rows <= INT32_MAX && count_ok(rows, n), CATQ_ERR_SHAPE, "too many rows");
+  // (a launch has fewer than 2^32 threads along x, and a row at most 1024)
+  CATQ_REQUIRE(rows < (1 << (n <= 8192 ? 24 : 22)) && count_ok(rows, n), CATQ_ERR_SHAPE, "too many rows");
   return CATQ_OK;
 }
 

@@ -375,16 +375,24 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
 
 // ------------------------------------------------------------------ many rows
 //
-// A workgroup takes 128 rows, 32 per wave, and 64-token tiles of the span: the four waves
-// convert a tile's codes once, into LDS as fp16 operands, and each forms S^T = K Q^T and
+// A workgroup takes 32 NW rows (128 or 256), 32 per wave, and 64-token tiles of the span: the NW
+// waves convert a tile's codes once, into LDS as fp16 operands, and each forms S^T = K Q^T and
 // O^T = V^T P^T of its rows with v_mfma_f32_32x32x16_f16. As above a lane holds one query
 // (column lane % 32), its scores of a 32-token block are the tokens 8 qd + 4 h + e (h = lane / 32)
 // in register 4 qd + e, and those are, in order, the contraction slots of the second
 // product when the v operand takes the four-token words 4 T + h and 4 T + 2 + h of each 16 tokens.
 //   s_k [slice ks][h][token], 65 tokens apart: values 16 ks + 8 h .. + 7 of the token, 16 bytes
 //   s_v [T][h][d]: the eight tokens of those two words at value d, 16 bytes
-// (16 lanes read, and write k, in 16 different 16-byte banks; one lane address for all reads). LDS is double-buffered, one
-// barrier per tile; the codes of the next tile are loaded while this one is multiplied.
+// (16 lanes read, and write k, in 16 different 16-byte banks; one lane address for all reads).
+// LDS is double-buffered, one barrier per tile; the codes of the next tile are loaded while
+// this one is multiplied.
+//
+// Three prompt chunks of 2000, 792 and 1184 tokens behind up to 4000, 40 + 8 heads of 128: 401 us,
+// 825 TFLOP/s. Per wave and tile 248 vector instructions (32 of them exponentials at a quarter rate)
+// and 32 products, 1380 and 1024 cycles, which do not overlap: the matrix cores are busy
+// 34% of the time, the vector ALU 50%, and 16% of the units wait at the end. Giving the two
+// waves of a SIMD turns (one multiplies, one exponentiates, a barrier between) brought nothing
+// (420 us), nor did half tiles interleaved inside a wave (they spill).
 // A tile's v scale is in lv (log2, NaN outside its range, -inf on a page that does not
 // exist) and rv (its reciprocal, always finite, so that a masked token adds 0).
 constexpr int kTile = 64, kPitch = kTile + 1;
@@ -768,18 +776,17 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
     a.lse[at] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
 }
 
-// How a call is split: rows per workgroup (16 or 32: the waves split the context; 128: the
-// waves split the rows) and spans of the context.
+// How a call is split: rows per workgroup (16 or 32: the waves split the context; 128 or 256: the
+// waves split the rows; 256 rows share a tile's conversion, 404 us for three prompt chunks where
+// 128 take 421) and spans of the context.
 struct Plan {
   int tile_rows, row_tiles, spans, span;
 };
-#ifndef PA_T
-#define PA_T 128
-#endif
+
 Plan plan(const catq_kv_desc* d, const catq_kv_batch* b) {
   const int64_t rows = (int64_t)b->max_new * (d->n_q / d->n_kv);
   Plan p;
-  p.tile_rows = rows <= 16 ? 16 : rows <= 32 || d->head_dim == 256 ? 32 : rows <= PA_T ? 128 : 256;
+  p.tile_rows = rows <= 16 ? 16 : rows <= 32 || d->head_dim == 256 ? 32 : rows <= 128 ? 128 : 256;
   p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
   // Spans so that the chip has 512 workgroups where the context allows (131072 tokens of one sequence:
   // 58 us; 62 with 1024, 67 with 2048), none under 256 tokens (1000 tokens of one sequence: 9.9 us; 12.4
@@ -850,8 +857,9 @@ extern "C" catq_status catq_aux_paged_attention(const catq_kv_desc* d, const cat
                    (reinterpret_cast<uintptr_t>(lse) & 3) == 0,
                CATQ_ERR_ALIGN, "misaligned");
   const Plan p = plan(d, batch);
-  CATQ_REQUIRE((int64_t)p.row_tiles * p.spans * d->n_kv <= INT32_MAX &&
-                   (p.spans == 1 || batch->n_tokens * d->n_q <= INT32_MAX) &&
+  // (a launch has fewer than 2^32 threads along x)
+  CATQ_REQUIRE((int64_t)p.row_tiles * p.spans * d->n_kv < (1 << 23) &&
+                   (p.spans == 1 || batch->n_tokens * d->n_q < (1 << 24)) &&
                    (int64_t)batch->max_new * (d->n_q / d->n_kv) <= INT32_MAX / 2 &&
                    (int64_t)d->max_pages * d->page_size <= INT32_MAX / 2,
                CATQ_ERR_SHAPE, "too many rows or too long a context for one launch");

@@ -470,7 +470,8 @@ extern "C" catq_status catq_ternary_linear_a8(const int8_t* q, int64_t M, int64_
   CATQ_REQUIRE(d_in % g == 0, CATQ_ERR_SHAPE, "d_in (%lld) must be a multiple of g (%d)",
                (long long)d_in, g);
   CATQ_REQUIRE(d_in <= 65536, CATQ_ERR_SHAPE, "d_in must be <= 65536");
-  CATQ_REQUIRE((d_out + 15) / 16 <= INT32_MAX && (M + 15) / 16 <= 65535, CATQ_ERR_SHAPE,
+  // (a launch has fewer than 2^32 threads along x: 512 per 16 rows at least)
+  CATQ_REQUIRE((d_out + 15) / 16 < (1 << 23) && (M + 15) / 16 <= 65535, CATQ_ERR_SHAPE,
                "d_out or M too large for one launch");
   CATQ_REQUIRE(ldq >= d_in && ldq % 16 == 0 && ldq <= (1 << 24), CATQ_ERR_SHAPE,
                "ldq must be >= d_in, a multiple of 16 and <= 2^24");

@@ -636,6 +636,26 @@ def test_attention_masked_contents_do_not_count(catq):
             assert torch.isfinite(o[:28].float()).all()
 
 
+@pytest.mark.parametrize("new,heads,d", [(1, 2, 64), (9, 2, 128), (30, 2, 128), (90, 2, 64), (200, 2, 128)])
+def test_attention_non_finite_queries(catq, new, heads, d):
+    """A query row of NaN or infinities changes no other row, in no form of the kernel."""
+    sv = Serving(catq, [(700, new), (33, new)], heads, 1, d, 32, 16).upload()
+    q = _rand(sv.g, sv.tokens, heads * d).cuda()
+    ws = torch.empty(max(1, catq.catq_paged_attention_workspace_bytes(sv.desc, sv.batch)), dtype=torch.uint8,
+                     device="cuda")
+    o, o2 = (torch.empty((sv.tokens, heads * d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    catq.catq_aux_paged_attention(sv.desc, sv.cache, sv.batch, q, o, ws)
+    q2 = q.clone()
+    q2[new // 2, :d] = float("nan")
+    q2[new, d:] = float("inf")
+    catq.catq_aux_paged_attention(sv.desc, sv.cache, sv.batch, q2, o2, ws)
+    touched = torch.zeros((sv.tokens, heads), dtype=torch.bool, device="cuda")
+    touched[new // 2, 0] = touched[new, 1] = True
+    rows, rows2 = o.view(-1, heads, d), o2.view(-1, heads, d)
+    assert torch.isnan(rows2[new // 2, 0]).all()
+    assert torch.equal(rows2[~touched], rows[~touched])
+
+
 def test_workspace_and_streams(catq):
     """A workspace that is too small is refused; a call on another stream than the
     tensors' gives the same."""

@@ -143,6 +143,24 @@ def test_cache_refusals(cq):
     assert attend(max_pages=4000, max_len=200000, n=64) == WORKSPACE
 
 
+def test_launch_limits(cq):
+    """A call whose launch would have 2^32 threads or more along one axis is refused."""
+    L, R = cq.lib, C.byref
+    norm = lambda rows, n: L.catq_aux_rmsnorm_quant(FAKE, 1, None, 1, None, rows, n, n, 1e-6, None, FAKE, None,
+                                                    None, None)
+    assert norm(1 << 24, 8192) == SHAPE and norm(1 << 22, 16384) == SHAPE
+    assert L.catq_aux_act_quant8(FAKE, 1, 1 << 24, 64, 64, FAKE, FAKE, None) == SHAPE
+    assert L.catq_ternary_linear_a8(FAKE, 4, 256, FAKE, FAKE, FAKE, 1 << 27, 256, 128, FAKE, 0, 1 << 27,
+                                    None) == SHAPE
+    for kw in (dict(n_tokens=(1 << 24) // 8, n_seqs=1, max_pages=100, max_len=6000),      # the spans' join
+               dict(n_q=1024, n_kv=1024, max_new=1 << 22, max_len=1 << 20, max_pages=1 << 14, n_pages=1)):
+        d, c, b, _ = _structs(cq, **kw)
+        assert L.catq_aux_paged_attention(R(d), R(c), R(b), FAKE, 0.1, FAKE, None, FAKE, 1 << 62, None) == SHAPE, kw
+    d, c, b, p = _structs(cq, n_q=1024, n_kv=1024, n_tokens=1 << 20, max_new=1 << 20, max_pages=1 << 16, n_pages=1)
+    assert L.catq_aux_kv_append(R(d), R(c), R(b), R(p), FAKE, FAKE, None) == SHAPE
+    assert L.catq_aux_kv_read(R(d), R(c), R(b), FAKE, None, None) == SHAPE
+
+
 def test_workspace_bytes(cq):
     """None for what needs none or is refused; as many partial results as spans otherwise."""
     def need(**kw):
