@@ -62,6 +62,13 @@ __device__ __forceinline__ i32x4 mfma_i8(u32x4 a, u32x4 b, i32x4 c) {
                                                0, 0, 0);
 }
 
+// the LDS reads of this wave have returned
+__device__ __forceinline__ void wait_lds() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#endif
+}
+
 template <typename OutT>
 __device__ __forceinline__ void store1(OutT* p, float v) {
   *p = (OutT)v;
@@ -79,18 +86,32 @@ __device__ __forceinline__ void static_for(F&& f) {
 constexpr int kBufferFlags = 0x00020000;  // raw buffer resource word 3 (gfx9 family)
 constexpr int kOutOfRange = 0x40000000;   // offset past every slice this kernel builds
 
-// Few tokens.  One workgroup = R tiles of 16 output rows x NT tiles of 16 tokens; its NW
-// waves take the 128-code chunks in turn and are added through LDS in a fixed order.  A
-// code is decoded once for all token tiles, a token's activations are brought into order once
-// for all row tiles.  A ring of D + 1 register slots keeps D chunks of every wave in flight;
-// the scales are staged in LDS once, loaded before the ring's first chunks and stored
-// after them.  XL (at most four tokens): the activations lie in LDS, in operand order.
+// Few tokens.  One workgroup = R tiles of 16 output rows x NT tiles of 16 tokens; each of its NW
+// waves takes a run of 128-code chunks, and they are added through LDS in a fixed order.  A code is
+// decoded once for all token tiles, a token's activations are brought into order once for all row
+// tiles.  Codes (two chunks at a time) and activations come by direct copies into LDS of each
+// wave's own (no barriers); their operands are read at once, and the next copies are issued into
+// the same place before the products.  A matrix operand has 16 neighbouring lanes in
+// 16 different rows, and loading it so, straight into registers, cost the L1 64 cycles an
+// instruction whatever its width; a copy's neighbouring lanes take 64 bytes of a row of codes, 128 of
+// a token, and LDS does the exchange (5120 x 17408: 19.0 -> 13 us at 16 tokens, 30.3 -> 18.4 at 48).
+// Within a row the 16-byte pieces are permuted, so that the operands' reads use all banks.
+//   codes of a row tile  [16 rows][4 pieces], piece p of row t at p ^ (t / 4)
+//   activations          [16 NT tokens][8 pieces], piece p of token t at p ^ (t / 2 % 8)
+// XL (at most four tokens): the activations lie in LDS as a whole, in operand order.
+//
+// What bounds it: at one token (34816 x 5120: 13.2 us) the codes, 10.5 us from HBM, behind 3 of
+// launch and first loads; with more the vector instructions (per chunk 16 a token tile, 22 a row tile,
+// 8 a pair of them: 7 of the 18 us at 48 tokens x 5120 x 17408 if all units had the same
+// share, but its 160 workgroups leave 96 of 256 idle).  A ring of two or three slots brought nothing,
+// and its LDS costs workgroups per unit (34816 x 5120 at 16: 20.3 us with two, 18.4 with one).
 // Dynamic LDS: groups * (RT + 4) floats, then with XL tokens * d_in bytes.
-template <int NW, int R, int NT, int D, bool XL, typename OutT>
+template <int NW, int R, int NT, bool XL, typename OutT>
 __global__ __launch_bounds__(NW * 64) void ternary_a8_gemv_kernel(A8Args a) {
-  constexpr int RT = 16 * R, AP = RT + 4, S = D + 1, T = NW * 64, AMAX = 16;
+  constexpr int RT = 16 * R, AP = RT + 4, T = NW * 64, AMAX = 128 / NW;
+  constexpr int WB = R * 1024, OWN = WB + (XL ? 0 : NT * 2048), RED = NW * 16 * (RT + 1) * 4;   // bytes
+  __shared__ __align__(16) char s_own[NW * OWN > RED ? NW * OWN : RED];
   extern __shared__ __align__(16) float s_alpha[];
-  __shared__ float s_red[NW][16][RT + 1];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q = lane >> 4, c16 = lane & 15;
@@ -99,6 +120,39 @@ __global__ __launch_bounds__(NW * 64) void ternary_a8_gemv_kernel(A8Args a) {
   const int64_t row_bytes = a.d_in >> 2;
   const int rows_here = (int)min<int64_t>(RT, a.d_out - n0);
   const int toks_here = (int)min<int64_t>(16 * NT, a.M - m0);
+  const int ch0 = wave * nch / NW, my = (wave + 1) * nch / NW - ch0;
+
+  // codes: a lane copies to piece lane % 4 of row lane / 4 of a tile; past the tile zeros
+  const i32x4_rsrc wr = buf_rsrc(a.P + n0 * row_bytes, (uint32_t)(rows_here * row_bytes));
+  uint32_t woff[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = 16 * r + (lane >> 2);
+    woff[r] = row < rows_here ? (uint32_t)(row * row_bytes) + ((lane & 3) ^ (lane >> 4)) * 16 + ch0 * 32 : kOutOfRange;
+  }
+  // activations: to piece lane % 8 of token lane / 8 of eight; past the last token zeros
+  const i32x4_rsrc xr = buf_rsrc(a.X + m0 * a.ldx, (uint32_t)((toks_here - 1) * a.ldx + a.d_in));
+  uint32_t xoff[2 * NT];
+#pragma unroll
+  for (int i = 0; i < 2 * NT; ++i) {
+    const int t = 8 * i + (lane >> 3);
+    xoff[i] = t < toks_here ? (uint32_t)(t * a.ldx) + ((lane & 7) ^ ((t >> 1) & 7)) * 16 : kOutOfRange;
+  }
+  const char* own = s_own + wave * OWN;
+  const uint32_t olds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_own + wave * OWN;
+  auto copy_w = [&](int k) __attribute__((always_inline)) {   // (past a row's end: the next row, or zeros; never used)
+#pragma unroll
+    for (int r = 0; r < R; ++r) dma16_lds(wr, woff[r] + (uint32_t)k * 32u, 0u, olds + r * 1024);
+  };
+  auto copy_x = [&](int k) __attribute__((always_inline)) {
+    if constexpr (!XL) {
+      const uint32_t ch = min(ch0 + k, nch - 1);   // (past the end: re-read, never used)
+#pragma unroll
+      for (int i = 0; i < 2 * NT; ++i) dma16_lds(xr, xoff[i] + ch * 128u, 0u, olds + WB + i * 1024);
+    }
+  };
+  copy_w(0);
+  copy_x(0);
 
   // scales of the tile: index u T + tid = row * ng + group; past the tile zero
   const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc(
@@ -106,64 +160,49 @@ __global__ __launch_bounds__(NW * 64) void ternary_a8_gemv_kernel(A8Args a) {
   float av[AMAX];
 #pragma unroll
   for (int u = 0; u < AMAX; ++u)
-    av[u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ar, (tid + T * u) * 4, 0, 0));
+    if (T * u < RT * ng)
+      av[u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ar, (tid + T * u) * 4, 0, 0));
   u32x4* s_x = reinterpret_cast<u32x4*>(s_alpha + ng * AP);
   if constexpr (XL) {
     const int slots = nch * 8;   // 16-byte pieces per token
     for (int i = tid; i < toks_here * slots; i += T) {
-      const int t = i / slots, sl = i - t * slots;
+      const int t = (i >= slots) + (i >= 2 * slots) + (i >= 3 * slots), sl = i - t * slots;
       s_x[i] = transpose16(*reinterpret_cast<const u32x4*>(a.X + (m0 + t) * a.ldx + sl * 16));
     }
   }
-  const __amdgpu_buffer_rsrc_t pr = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint8_t*>(a.P + n0 * row_bytes), 0, (int)(rows_here * row_bytes), kBufferFlags);
-  int poff[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-    poff[r] = 16 * r + c16 < rows_here ? (int)((16 * r + c16) * row_bytes + 8 * q) : kOutOfRange;
-  const int8_t* xp[NT];   // (a token past the last reads the last's: its results are not stored)
-#pragma unroll
-  for (int t = 0; t < NT; ++t) xp[t] = a.X + min(m0 + 16 * t + c16, a.M - 1) * a.ldx + 32 * q;
-
-  const int my = wave < nch ? (nch - wave + NW - 1) / NW : 0;
-  const int last = my > 0 ? wave + NW * (my - 1) : 0;
-  uint2 cw[S][R];
-  [[maybe_unused]] u32x4 xv[S][NT][2];
-  auto issue = [&](int k, auto slot_c) __attribute__((always_inline)) {
-    constexpr int s = decltype(slot_c)::value;
-    const int ch = min(wave + NW * k, last);   // (past the end: re-read, never multiplied)
-    if constexpr (!XL) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          xv[s][t][j] = *reinterpret_cast<const u32x4*>(xp[t] + (int64_t)ch * 128 + 16 * j);
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      cw[s][r] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(pr, poff[r], ch * 32, 0));
-  };
-  static_for<0, D>([&](auto I) {
-    issue(I(), I);
-    __builtin_amdgcn_sched_barrier(0);
-  });
+  // (the division in fp32: a quotient of at most 8192 / ng is a half / ng or more from an integer.  As an
+  // integer division, and for all of AMAX, this took 3 us)
+  const float inv_ng = 1.0f / (float)ng;
 #pragma unroll
   for (int u = 0; u < AMAX; ++u) {
-    const int idx = tid + T * u, r = idx / ng;
+    if (T * u >= RT * ng) break;
+    const int idx = tid + T * u, r = (int)(((float)idx + 0.5f) * inv_ng);
     if (r < RT) s_alpha[(idx - r * ng) * AP + r] = av[u];
   }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+  wait_vmem();
+  __syncthreads();
 
   f32x4 out[NT][R];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int r = 0; r < R; ++r) out[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto compute = [&](int k, auto slot_c) __attribute__((always_inline)) {
-    constexpr int i = decltype(slot_c)::value;
-    const int ch = wave + NW * k;
+  const int wrd = c16 * 64 + 8 * (q & 1), wsw = c16 >> 2;
+  const int xrd = WB + c16 * 128, xsw = (c16 >> 1) & 7;
+  uint2 cw[2][R];
+  auto step = [&](int k, auto par_c) __attribute__((always_inline)) {
+    constexpr int par = decltype(par_c)::value;   // k & 1
+    const int ch = ch0 + k;
+    // (in order of their issue: activations of k, then with odd k the codes of k + 1 and k + 2)
+    if constexpr (par == 0) wait_vmem();
+    else if constexpr (!XL) wait_vmem_n<R>();
+    if constexpr (par == 0) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          cw[p][r] = *reinterpret_cast<const uint2*>(own + r * 1024 + wrd + ((2 * p + (q >> 1)) ^ wsw) * 16);
+    }
     u32x4 xf[NT][2];
     if constexpr (XL) {
       const u32x4* p = s_x + (min(c16, toks_here - 1) * nch + ch) * 8 + 2 * q;
@@ -173,36 +212,43 @@ __global__ __launch_bounds__(NW * 64) void ternary_a8_gemv_kernel(A8Args a) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) xf[t][j] = transpose16(xv[i][t][j]);
+        for (int j = 0; j < 2; ++j)
+          xf[t][j] = *reinterpret_cast<const u32x4*>(own + t * 2048 + xrd + ((2 * q + j) ^ xsw) * 16);
     }
     const float* al = &s_alpha[(ch >> a.cpg_shift) * AP + 4 * q];
+    f32x4 sc[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) sc[r] = *reinterpret_cast<const f32x4*>(al + 16 * r);
+    if (!XL || par == 0) wait_lds();   // what was read may be written over
+    copy_x(k + 1);
+    if constexpr (par == 0) copy_w(k + 2);
+    if constexpr (!XL) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) xf[t][j] = transpose16(xf[t][j]);
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const u32x4 w0 = decode16_i8(cw[i][r].x), w1 = decode16_i8(cw[i][r].y);
-      const f32x4 sc = *reinterpret_cast<const f32x4*>(al + 16 * r);
+      const u32x4 w0 = decode16_i8(cw[par][r].x), w1 = decode16_i8(cw[par][r].y);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         i32x4 acc = {0, 0, 0, 0};
         acc = mfma_i8(w0, xf[t][0], acc);
         acc = mfma_i8(w1, xf[t][1], acc);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[t][r][e] = fmaf(sc[e], (float)acc[e], out[t][r][e]);
+        for (int e = 0; e < 4; ++e) out[t][r][e] = fmaf(sc[r][e], (float)acc[e], out[t][r][e]);
       }
     }
   };
-  const int full = my / S * S;
-  for (int k0 = 0; k0 < full; k0 += S) {
-    static_for<0, S>([&](auto I) {
-      constexpr int i = I();
-      issue(k0 + i + D, std::integral_constant<int, (i + D) % S>{});
-      __builtin_amdgcn_sched_barrier(0);
-      compute(k0 + i, I);
-    });
+  for (int k = 0; k < my; k += 2) {
+    step(k, std::integral_constant<int, 0>{});
+    if (k + 1 < my) step(k + 1, std::integral_constant<int, 1>{});
   }
-  static_for<0, S - 1>([&](auto I) {
-    if (full + I() < my) compute(full + I(), I);
-  });
+  wait_vmem();     // (the last copies, never read: their place takes the sums)
+  __syncthreads();
 
+  auto s_red = reinterpret_cast<float (*)[16][RT + 1]>(s_own);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (t > 0) __syncthreads();
@@ -396,24 +442,34 @@ struct A8Work {
   double flops, bytes;
 };
 
-template <int NW, int R, int NT, int D>
+// LDS of a unit; a launch's scales, the waves' own places (or the reduction's)
+constexpr size_t kLds = 160 * 1024;
+template <int NW, int R, int NT>
+constexpr size_t gemv_lds(int ng, bool xl) {
+  const size_t own = NW * 1024 * (R + (xl ? 0 : 2 * NT)), red = sizeof(float) * NW * 16 * (16 * R + 1);
+  return (size_t)ng * (16 * R + 4) * sizeof(float) + std::max(own, red);
+}
+// every scale of a tile has a register of some thread, and the LDS suffices
+template <int NW, int R, int NT>
+constexpr bool gemv_fits(int ng) {
+  return ng * 16 * R <= 8192 && gemv_lds<NW, R, NT>(ng, false) <= kLds;
+}
+
+template <int NW, int R, int NT>
 catq_status launch_gemv(const A8Args& a, catq_dtype y_dtype, const A8Work& w, hipStream_t stream) {
   constexpr int RT = 16 * R;
   const int ng = a.n_chunks >> a.cpg_shift;
   const dim3 grid((unsigned)((a.d_out + RT - 1) / RT), (unsigned)((a.M + 16 * NT - 1) / (16 * NT)));
-  size_t lds = (size_t)ng * (RT + 4) * sizeof(float);
-  // every scale of a tile has a register, and the LDS stays within 64 KB
-  CATQ_REQUIRE(ng * RT <= 16 * NW * 64 && lds + sizeof(float) * NW * 16 * (RT + 1) <= 65536, CATQ_ERR_SHAPE,
-               "ternary_linear_a8: no launch shape for d_in = %lld", (long long)a.d_in);
+  size_t lds = (size_t)ng * (RT + 4) * sizeof(float);   // (dynamic; the rest is static)
   const size_t lds_x = (size_t)a.M * (size_t)a.d_in;
-  const bool xl = NT == 1 && a.M <= 4 && lds + lds_x + sizeof(float) * NW * 16 * (RT + 1) <= 65536;
+  const bool xl = NT == 1 && a.M <= 4 && gemv_lds<NW, R, NT>(ng, true) + lds_x <= kLds;
   if (xl) lds += lds_x;
   static char tag[64];
   trace_tag(tag, sizeof tag, "ternary_a8_gemv_kernel<%d, %d, %d%s>", NW, R, NT, xl ? ", x in lds" : "");
   auto launch = [&](auto xl_c, auto out_c) {
     using OutT = typename decltype(out_c)::type;
     CATQ_TRACED(stream, tag, w.flops, w.bytes, a.M, a.d_out, a.d_in,
-                hipLaunchKernelGGL((ternary_a8_gemv_kernel<NW, R, NT, D, decltype(xl_c)::value, OutT>), grid,
+                hipLaunchKernelGGL((ternary_a8_gemv_kernel<NW, R, NT, decltype(xl_c)::value, OutT>), grid,
                                    dim3(NW * 64), lds, stream, a));
   };
   auto with = [&](auto out_c) {
@@ -485,31 +541,43 @@ extern "C" catq_status catq_ternary_linear_a8(const int8_t* q, int64_t M, int64_
   const A8Work w{2.0 * (double)M * (double)d_out * (double)d_in,
                  (double)d_out * (double)d_in / 4.0 + 4.0 * (double)d_out * (double)(d_in / g) +
                      (double)M * (double)d_in + (double)M * (double)d_out * (double)dtype_size(y_dtype)};
-  // Which kernel: the least of a cost model in microseconds, fitted on MI355X.  A workgroup of
-  // the kernel for few tokens takes as long per eight chunks as the table says
-  // (rows and tokens in tiles of 16; at most four tokens lie in LDS), a compute unit takes
-  // its workgroups one after the other, and a launch costs 3.  The tiled kernel's workgroups (128
-  // rows x 64 tokens) take 0.42 per chunk, a lone one 0.72.  34816 x 5120: R = 3 at one
-  // token (14.7 us; 19.8 for R = 2), 16 (21.4; 34.5) and 32 (28.3 for 32 tokens at once; 39.3 for 16),
-  // tiled from 48 (38.4; 43.9).  5120 x 17408: R = 2 to 16 tokens (11.8, 18.9), R = 3 on 32 tokens
-  // at once at 48 (30.4; 33.1 for R = 2 on 48), on 64 at 100 (46.9; tiled 85.9).
+  // Which kernel: the least of a cost model in microseconds, fitted on MI355X over 56 sizes (1024 x 5120
+  // to 100000 x 2048, one token to 100; its choice is 3% behind the best of 15 on average, 14% at
+  // worst).  A launch costs base; then per chunk a workgroup alone on its compute unit takes alone,
+  // and several of them each apiece.  5120 x 17408: R = 1 at one token (9.1 us; 13.7 for R = 2), R = 2
+  // with three token tiles at 48 (19.9; 21.3 with one, 24.6 with two).  34816 x 5120: R = 2 on four waves at one
+  // token (13.3; 14.4 for R = 1), R = 3 on four waves with two token tiles at 48 (32.2; tiled 38.2), tiled from 64.
+  // 8192 x 8192 at 16: R = 1 (8.4; 9.9 for R = 2 with two token tiles).
   const int ng = a.n_chunks >> a.cpg_shift;
-  if (ng > 256) return launch_gemv<8, 1, 1, 3>(a, y_dtype, w, stream);   // (scales: one per thread register)
-  const bool few = M <= 4;
-  const double t21 = few ? 0.60 : 0.95, t31 = few ? 0.78 : 1.2;
-  auto gemv = [&](int r, int nt, double t) {
-    const double wgs = std::ceil((double)d_out / (16 * r)) * std::ceil((double)M / (16 * nt));
-    return r == 3 && ng > 170 ? 1e300 : 3.0 + a.n_chunks / 8.0 * std::ceil(wgs / 256.0) * t;
+  struct Choice {
+    int rows, tokens;
+    double base, alone, each;
+    bool fits;
   };
-  const double cost[6] = {gemv(2, 1, t21), gemv(3, 1, t31), gemv(2, 2, 1.31), gemv(3, 2, 1.65), gemv(3, 4, 2.7),
-                          4.0 + a.n_chunks * std::max(0.72, 0.42 * std::ceil(std::ceil(d_out / 128.0) *
-                                                                             std::ceil(M / 64.0) / 256.0))};
-  switch (std::min_element(cost, cost + 6) - cost) {
-    case 0: return launch_gemv<8, 2, 1, 3>(a, y_dtype, w, stream);
-    case 1: return launch_gemv<8, 3, 1, 2>(a, y_dtype, w, stream);
-    case 2: return launch_gemv<8, 2, 2, 2>(a, y_dtype, w, stream);
-    case 3: return launch_gemv<8, 3, 2, 1>(a, y_dtype, w, stream);
-    case 4: return launch_gemv<8, 3, 4, 1>(a, y_dtype, w, stream);
+  const Choice choices[6] = {{16, 16, 3.2, 0.049, 0.041, gemv_fits<8, 1, 1>(ng)},
+                             {32, 16, 3.2, 0.091, 0.060, gemv_fits<4, 2, 1>(ng)},
+                             {32, 32, 3.3, 0.094, 0.100, gemv_fits<8, 2, 2>(ng)},
+                             {32, 48, 3.8, 0.115, 0.131, gemv_fits<8, 2, 3>(ng)},
+                             {48, 32, 4.0, 0.148, 0.122, gemv_fits<4, 3, 2>(ng)},
+                             {128, 64, 5.7, 0.58, 0.39, true}};
+  int best = 5;
+  double least = 1e300;
+  for (int i = 0; i < 6; ++i) {
+    const Choice& c = choices[i];
+    if (!c.fits) continue;
+    const double wgs = std::ceil((double)d_out / c.rows) * std::ceil((double)M / c.tokens);
+    const double cost = c.base + a.n_chunks * (wgs <= 256 ? c.alone : c.each * std::ceil(wgs / 256.0));
+    if (cost < least) {
+      least = cost;
+      best = i;
+    }
+  }
+  switch (best) {
+    case 0: return launch_gemv<8, 1, 1>(a, y_dtype, w, stream);
+    case 1: return launch_gemv<4, 2, 1>(a, y_dtype, w, stream);
+    case 2: return launch_gemv<8, 2, 2>(a, y_dtype, w, stream);
+    case 3: return launch_gemv<8, 2, 3>(a, y_dtype, w, stream);
+    case 4: return launch_gemv<4, 3, 2>(a, y_dtype, w, stream);
     default: return launch_gemm<4, 2>(a, y_dtype, w, stream);
   }
 }

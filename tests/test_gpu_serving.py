@@ -186,6 +186,23 @@ def test_linear_a8(catq, M, d_out, d_in, g):
         assert torch.equal(Y, Z)
 
 
+@pytest.mark.parametrize("M,d_out,d_in,g", [
+    (3, 4111, 2176, 128), (3, 8203, 5248, 128), (13, 8203, 5248, 128), (21, 4111, 2176, 128), (33, 34001, 896, 128),
+    (45, 16421, 2176, 128), (45, 16421, 2304, 256), (1000, 16421, 128, 128), (257, 16421, 896, 128),
+    (500, 8203, 2176, 128), (1000, 4111, 2304, 256)])
+def test_linear_a8_many_rows(catq, M, d_out, d_in, g):
+    """The launch shapes for many rows, the last tile of rows and of tokens cut off, strided; the rows
+    behind as they were."""
+    q, packed, alpha, xs = _linear_inputs(M, d_out, d_in, g, M + d_out)
+    wide = torch.full((M, d_in + 16), 77, dtype=torch.int8, device="cuda")
+    wide[:, :d_in] = q.cuda()
+    out = torch.full((M + 1, d_out + 3), 5.0, device="cuda")
+    catq.catq_ternary_linear_a8(wide[:, :d_in], xs.cuda(), packed.cuda(), alpha.cuda(), out[:M, :d_out],
+                              g=g)
+    _linear_check(out[:M, :d_out], q, packed, alpha, xs, g, False)
+    assert (out[:, d_out:] == 5.0).all() and (out[M] == 5.0).all()
+
+
 @pytest.mark.parametrize("M", [3, 20, 150])
 def test_linear_a8_strided_rows(catq, M):
     d_out, d_in = 70, 512
