@@ -462,7 +462,7 @@ typedef struct {
 } catq_kv_batch;
 typedef struct {
   const float* inv_freq;  /* fp32 [rot_dim/2]: pair i of position p turns by p * inv_freq[i]
-                             (formed in float64); any scaling of the frequencies for
+                             (to 2^-25 of a turn or better); any scaling of the frequencies for
                              long contexts is in them.  NULL if rot_dim is 0          */
   const void* q_weight;   /* bf16 [head_dim] gain of the q norm, NULL for ones        */
   const void* k_weight;

@@ -26,6 +26,11 @@
 // therefore held to [2^-60, 2^30], where that cannot be.
 // The running maximum is only raised when a score exceeds it by 2^8 (p' <= 256 is as good
 // in fp16 as p' <= 1), so the rescaling of the output is rare.
+//
+// What bounds it: the codes from HBM where the context is long (64 sequences of up to 8192 tokens, 8 kv
+// heads of 128: 131 us, 4.5 TB/s; vector ALU 32%, matrix cores 6%), and where it is
+// short one chain of latencies (lengths, page, codes, join): 7.5 us at 300 tokens. One
+// sequence of 131072 tokens: 46 us and 4 for the join of its 64 spans a head (58 us together with the gap).
 #include <algorithm>
 #include <type_traits>
 

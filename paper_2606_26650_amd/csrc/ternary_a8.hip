@@ -280,10 +280,11 @@ __global__ __launch_bounds__(NW * 64) void ternary_a8_gemv_kernel(A8Args a) {
 // chunk's values 64 h .. 64 h + 63, in four contraction steps of v_mfma_i32_32x32x32_i8.  The sums of
 // a chunk are converted and added with the rows' scales; with larger groups only once a group.
 //
-// 1000 x 34816 x 5120: 284 us, 1.26 PFLOP/s.  What bounds it is the sum of what one compute
-// unit does per chunk: the LDS reads of the operands (50% of its bandwidth), 37% of the vector
-// issue (decode, conversion, scaling) and 21% of the matrix cores, four waves per SIMD overlapping
-// them; leaving out any one of them gains 5-15%, the activations' staging 18%.
+// 1000 x 34816 x 5120: 280-290 us, 1.25 PFLOP/s, at a clock of 1.9 GHz.  What bounds it is the
+// vector instructions: 145 per wave and chunk (64 convert and scale the sums, 44 decode, 16 bring
+// activations into order) take 72% of the issue cycles, beside matrix cores at 32% and the LDS
+// reads of the operands at half of its bandwidth, four waves per SIMD overlapping them; leaving
+// out any one of them gains 5-15%, the activations' staging 18%.
 template <int NWV, int CB, bool G128, typename OutT>
 __global__ __launch_bounds__(NWV * 64, 4) void ternary_a8_gemm_kernel(A8Args a) {
   constexpr int T = NWV * 64, RT = 32 * NWV, TT = 32 * CB;
