@@ -429,6 +429,44 @@ def test_append_far_positions(catq):
         assert (err <= BF * want.abs() + 4 * FP * want.abs().max()).all()
 
 
+def test_pool_past_32_bits(catq):
+    """Pages more than 2^32 bytes into the pool: the same as in a small one."""
+    c, n_q, n_kv, d, ps, bt, width = catq, 16, 8, 128, 256, 16, 3
+    i32 = dict(dtype=torch.int32, device="cuda")
+    g = _gen(11)
+    seqs = [(250, 200), (511, 1), (0, 40)]
+    n = sum(s[1] for s in seqs)
+    x = _rand(g, n, (n_q + 2 * n_kv) * d).cuda()
+    old = _rand(g, 761, (n_q + 2 * n_kv) * d).cuda()
+    inv = (1e4 ** (-torch.arange(64) / 64)).float().cuda()
+    got = []
+    for pages in (9, 20480):                             # 2^18 bytes each: 5 GB
+        k = torch.empty((pages, n_kv, ps, d), dtype=torch.int8, device="cuda")
+        v = torch.empty((pages, n_kv, ps // 4, d, 4), dtype=torch.int8, device="cuda")
+        ks, vs = (torch.zeros((pages, n_kv, ps // bt), device="cuda") for _ in range(2))
+        desc = c.kv_desc(n_q, n_kv, d, ps, bt, pages, width)
+        cache, prep = c.kv_cache(desc, k, v, ks, vs), c.kv_prep(desc, inv, rot_dim=d, qk_norm=True)
+        table = torch.arange(pages - 1, pages - 10, -1, **i32).view(3, width)
+        first = c.kv_batch(desc, table, torch.tensor([0, 250, 761, 761], **i32), torch.zeros(3, **i32), 761, 511, 511)
+        q = torch.empty((761, n_q * d), dtype=torch.bfloat16, device="cuda")
+        c.catq_aux_kv_append(desc, cache, first, prep, old, q)
+        out = [q]
+        for part in ([0, 200, 201, 241], [0, 1, 2, 3]):      # tiles of many rows, single tokens
+            b = c.kv_batch(desc, table, torch.tensor(part, **i32), torch.tensor([s[0] for s in seqs], **i32), part[-1],
+                           max(part[i + 1] - part[i] for i in range(3)), 512)
+            q, o = (torch.zeros((part[-1], n_q * d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            kv = [torch.zeros((part[-1], n_kv * d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+            ws = torch.empty(max(1, c.catq_paged_attention_workspace_bytes(desc, b)), dtype=torch.uint8, device="cuda")
+            c.catq_aux_kv_append(desc, cache, b, prep, x[:part[-1]].contiguous(), q)
+            c.catq_aux_kv_read(desc, cache, b, *kv)
+            c.catq_aux_paged_attention(desc, cache, b, q, o, ws)
+            out += [q, o, *kv]
+        got.append(out)
+    assert pages * n_kv * ps * d > 2 ** 32
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
 def test_append_leaves_the_rest(catq):
     """Codes and scales that no new token touches keep their bits: older blocks, later
     tokens of the page, other pages, blocks of other heads."""
