@@ -268,7 +268,7 @@ __global__ __launch_bounds__(NW * 64) void ternary_a8_gemv_kernel(A8Args a) {
   }
 }
 
-// Many tokens.  One workgroup = 32 NWV weight rows x 32 CB tokens (128 x 64); each of its NWV
+// Many tokens.  One workgroup = 32 NWV weight rows x 32 CB tokens (128 or 256 x 64); each of its NWV
 // waves takes 32 rows and all the tokens, so a code is decoded once per workgroup.  Per 128-code
 // chunk the tokens' activations go through registers (where they are brought into operand order;
 // loaded two chunks ahead) into a double-buffered LDS tile [token][8 slots of 16 bytes], slot s of
@@ -280,9 +280,9 @@ __global__ __launch_bounds__(NW * 64) void ternary_a8_gemv_kernel(A8Args a) {
 // chunk's values 64 h .. 64 h + 63, in four contraction steps of v_mfma_i32_32x32x32_i8.  The sums of
 // a chunk are converted and added with the rows' scales; with larger groups only once a group.
 //
-// 1000 x 34816 x 5120: 280-290 us, 1.25 PFLOP/s, at a clock of 1.9 GHz.  What bounds it is the
+// 1000 x 34816 x 5120: 275 us, 1.3 PFLOP/s, at a clock of 1.9 GHz.  What bounds it is the
 // vector instructions: 145 per wave and chunk (64 convert and scale the sums, 44 decode, 16 bring
-// activations into order) take 72% of the issue cycles, beside matrix cores at 32% and the LDS
+// activations into order, 8 with eight waves) take 72% of the issue cycles, beside matrix cores at 32% and the LDS
 // reads of the operands at half of its bandwidth, four waves per SIMD overlapping them; leaving
 // out any one of them gains 5-15%, the activations' staging 18%.
 template <int NWV, int CB, bool G128, typename OutT>
@@ -579,6 +579,11 @@ extern "C" catq_status catq_ternary_linear_a8(const int8_t* q, int64_t M, int64_
     case 2: return launch_gemv<8, 2, 2>(a, y_dtype, w, stream);
     case 3: return launch_gemv<8, 2, 3>(a, y_dtype, w, stream);
     case 4: return launch_gemv<4, 3, 2>(a, y_dtype, w, stream);
-    default: return launch_gemm<4, 2>(a, y_dtype, w, stream);
+    default:
+      // Eight waves share the activations of a tile where 1024 workgroups or more are left, four to a
+      // unit (1000 x 34816 x 5120: 275 us, 288 with four waves; 4000 x 5120 x 5120: 163, 170; but 1000 x 5120
+      // x 17408, 320 workgroups: 170, 157).
+      if (std::ceil(d_out / 256.0) * std::ceil(M / 64.0) >= 1024) return launch_gemm<8, 2>(a, y_dtype, w, stream);
+      return launch_gemm<4, 2>(a, y_dtype, w, stream);
   }
 }

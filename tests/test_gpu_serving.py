@@ -189,7 +189,7 @@ def test_linear_a8(catq, M, d_out, d_in, g):
 @pytest.mark.parametrize("M,d_out,d_in,g", [
     (3, 4111, 2176, 128), (3, 8203, 5248, 128), (13, 8203, 5248, 128), (21, 4111, 2176, 128), (33, 34001, 896, 128),
     (45, 16421, 2176, 128), (45, 16421, 2304, 256), (1000, 16421, 128, 128), (257, 16421, 896, 128),
-    (500, 8203, 2176, 128), (1000, 4111, 2304, 256)])
+    (500, 8203, 2176, 128), (1000, 4111, 2304, 256), (4090, 4111, 896, 128), (8200, 2049, 768, 256)])
 def test_linear_a8_many_rows(catq, M, d_out, d_in, g):
     """The launch shapes for many rows, the last tile of rows and of tokens cut off, strided; the rows
     behind as they were."""
