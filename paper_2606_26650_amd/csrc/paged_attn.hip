@@ -810,7 +810,7 @@ Plan plan(const catq_kv_desc* d, const catq_kv_batch* b) {
 template <int D>
 catq_status launch_paged(const PaArgs& a, bool per_token, double flops, double bytes, hipStream_t stream) {
   const dim3 grid((unsigned)((int64_t)a.row_tiles * a.spans * a.g.n_kv), (unsigned)a.g.n_seqs);
-  static char tag[64];
+  char tag[64];
   trace_tag(tag, sizeof tag, "paged_attn<%d rows, head_dim %d>", a.tile_rows, D);
   auto go = [&](auto kernel) {
     CATQ_TRACED(stream, tag, flops, bytes, a.g.n_tokens, a.g.n_q, D,

@@ -465,7 +465,7 @@ catq_status launch_gemv(const A8Args& a, catq_dtype y_dtype, const A8Work& w, hi
   const size_t lds_x = (size_t)a.M * (size_t)a.d_in;
   const bool xl = NT == 1 && a.M <= 4 && gemv_lds<NW, R, NT>(ng, true) + lds_x <= kLds;
   if (xl) lds += lds_x;
-  static char tag[64];
+  char tag[64];
   trace_tag(tag, sizeof tag, "ternary_a8_gemv_kernel<%d, %d, %d%s>", NW, R, NT, xl ? ", x in lds" : "");
   auto launch = [&](auto xl_c, auto out_c) {
     using OutT = typename decltype(out_c)::type;
@@ -488,7 +488,7 @@ catq_status launch_gemv(const A8Args& a, catq_dtype y_dtype, const A8Work& w, hi
 template <int NWV, int CB>
 catq_status launch_gemm(const A8Args& a, catq_dtype y_dtype, const A8Work& w, hipStream_t stream) {
   const dim3 grid((unsigned)((a.d_out + 32 * NWV - 1) / (32 * NWV)), (unsigned)((a.M + 32 * CB - 1) / (32 * CB)));
-  static char tag[64];
+  char tag[64];
   trace_tag(tag, sizeof tag, "ternary_a8_gemm_kernel<%d, %d>", NWV, CB);
   auto launch = [&](auto g128, auto out_c) {
     using OutT = typename decltype(out_c)::type;
