@@ -472,7 +472,7 @@ def kv_prep(desc, inv_freq=None, rot_dim=0, interleaved=False, qk_norm=False, q_
             _want(t, name, torch.bfloat16, (desc.head_dim,), dev)
     p = KvPrep(_ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), rot_dim, int(bool(interleaved)),
                int(bool(qk_norm)), int(bool(act_quant)), rope_scale, eps)
-    p.tensors, p.device = (inv_freq, q_weight, k_weight), dev
+    p.tensors, p.device, p.width = (inv_freq, q_weight, k_weight), dev, desc.head_dim
     return p
 
 
@@ -493,6 +493,8 @@ def catq_aux_kv_append(desc, cache, batch, prep, qkv, q_out, stream=None):
     dev, n, d = _kv_same(desc, cache, batch), batch.n_tokens, desc.head_dim
     if prep.device is not None and prep.device != dev:
         raise ValueError(f"prep: on GPU {prep.device}, expected {dev}")
+    if prep.width != d:
+        raise ValueError(f"prep: made for heads of {prep.width} values, expected {d}")
     _want(qkv, "qkv", torch.bfloat16, (n, (desc.n_q + 2 * desc.n_kv) * d), dev)
     _want(q_out, "q_out", torch.bfloat16, (n, desc.n_q * d), dev)
     _run_on(dev, stream, lib.catq_aux_kv_append, "catq_aux_kv_append", C.byref(desc), C.byref(cache),

@@ -467,6 +467,19 @@ def test_pool_past_32_bits(catq):
         assert torch.isfinite(a).all() and torch.equal(a, b)
 
 
+def test_append_refuses_another_heads_preparation(catq):
+    """Gains for heads of 64 values are not read as gains of 128."""
+    sv = Serving(catq, [(0, 2)], 2, 1, 128, 16, 16).upload()
+    small = catq.kv_desc(2, 1, 64, 16, 16, sv.desc.n_pages, sv.desc.max_pages)
+    prep = catq.kv_prep(small, torch.ones(32, device="cuda"), rot_dim=64, qk_norm=True,
+                        q_weight=torch.ones(64, dtype=torch.bfloat16, device="cuda"))
+    x = torch.zeros((sv.tokens, 4 * 128), dtype=torch.bfloat16, device="cuda")
+    q = torch.full((sv.tokens, 2 * 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="heads of 64"):
+        catq.catq_aux_kv_append(sv.desc, sv.cache, sv.batch, prep, x, q)
+    assert (q == 3.0).all()
+
+
 def test_append_leaves_the_rest(catq):
     """Codes and scales that no new token touches keep their bits: older blocks, later
     tokens of the page, other pages, blocks of other heads."""
