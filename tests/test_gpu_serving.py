@@ -215,6 +215,17 @@ def test_linear_a8_strided_rows(catq, M):
     assert (out[:, d_out:] == 5.0).all()
 
 
+@pytest.mark.parametrize("M,d_out,d_in", [(3, 100, 640), (33, 34001, 896), (70, 200, 640)])
+def test_linear_a8_far_rows(catq, M, d_out, d_in):
+    """Rows of activations 2^24 apart, the largest stride: offsets past 2^29."""
+    q, packed, alpha, xs = _linear_inputs(M, d_out, d_in, 128, M + d_in)
+    far = torch.empty((M, 1 << 24), dtype=torch.int8, device="cuda")[:, :d_in]
+    far.copy_(q)
+    out = torch.empty((M, d_out), device="cuda")
+    catq.catq_ternary_linear_a8(far, xs.cuda(), packed.cuda(), alpha.cuda(), out)
+    _linear_check(out, q, packed, alpha, xs, 128, False)
+
+
 def test_linear_a8_extremes(catq):
     """Every code at its largest: the integer sums of a group do not overflow, and one
     group of 65536 is exact."""
