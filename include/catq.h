@@ -462,8 +462,9 @@ typedef struct {
 } catq_kv_batch;
 typedef struct {
   const float* inv_freq;  /* fp32 [rot_dim/2]: pair i of position p turns by p * inv_freq[i]
-                             (to 2^-25 of a turn or better); any scaling of the frequencies for
-                             long contexts is in them.  NULL if rot_dim is 0          */
+                             (to 2^-25 of a turn, at any position); any scaling of the
+                             frequencies for long contexts is in them.  Below 2^20 in
+                             magnitude (others give NaN).  NULL if rot_dim is 0       */
   const void* q_weight;   /* bf16 [head_dim] gain of the q norm, NULL for ones        */
   const void* k_weight;
   int32_t rot_dim;        /* leading values of a head that rotate: a multiple of 16, 0 ..

@@ -86,28 +86,36 @@ struct AppendArgs {
   int32_t q_parts;      // workgroups per token for the query heads
 };
 
+// The turns of one position, inv_freq / 2 pi, as a 64-bit fraction of a turn (whole turns are left
+// out, which is what makes it exact for far positions: an integer times it, modulo 2^64, is
+// the fraction for that position).  1 / 2 pi is taken in two float64, of 2^-108 together, and the
+// product as a float64 and its error, so with |f| < 2^20 the fraction is off by less than 2^-63.
+__device__ __forceinline__ uint64_t turn_fraction(float f) {
+#pragma clang fp contract(off)   // (hi is the rounded product, also where it is subtracted from)
+  const double x = f, h = 0x1.45f306dc9c883p-3, l = -0x1.6b01ec5417056p-57;
+  const double hi = x * h, lo = fma(x, l, fma(x, h, -hi));
+  double frac = hi - rint(hi);                 // exact, within a half
+  if (frac >= 0.5) frac -= 1.0;
+  return (uint64_t)(int64_t)(frac * 0x1p64) + (uint64_t)(int64_t)(int)rint(lo * 0x1p64);
+}
+
 // cos and sin of `n` positions from pos0 on, times the scale, at cs[t][rot/2]: by one wave, a
-// lane per frequency. The turns are pos * inv_freq / 2 pi with the factor in two floats (of
-// 48 bits together, from float64), less the whole ones inside an fma: off by 2^-25 of a turn
-// below position 2^24, in five operations where float64 takes a hundred cycles; float64 beyond.
+// lane per frequency.  The fraction's upper 32 bits round to fp32 by 2^-26 of a turn, all
+// else is below 2^-31.  (Two floats with the whole turns taken off in an fma take the same time, 56 us
+// for the prompts above with their read back, and were off by 2^-24, more at frequencies above 1.)
+// Frequencies of 2^20 and above, infinite and NaN ones give NaN.
 __device__ __forceinline__ void angles(const AppendArgs& a, int64_t pos0, int n, float2* cs) {
   const int half = a.rot >> 1;
   for (int f = threadIdx.x & 63; f < half; f += 64) {
-    const double turn = (double)a.inv_freq[f] * 0.15915494309189533577;
-    const float hi = (float)turn, lo = (float)(turn - (double)hi);
-    for (int t = 0; t < n; ++t) {
-      const int64_t pos = pos0 + t;
-      float r;
-      if (pos < (1 << 24)) {
-        const float x = (float)pos, whole = rintf(x * hi);
-        r = fmaf(x, lo, fmaf(x, hi, -whole));
-      } else {
-        const double p = (double)pos * turn;
-        r = (float)(p - rint(p));
-      }
+    const float freq = a.inv_freq[f];
+    const bool fine = fabsf(freq) < 0x1p20f;
+    const float scale = fine ? a.rope_scale : __builtin_nanf("");
+    const uint64_t turn = turn_fraction(fine ? freq : 0.f);
+    uint64_t at = turn * (uint64_t)pos0;
+    for (int t = 0; t < n; ++t, at += turn) {
       float s, c;
-      sincospif(2.0f * r, &s, &c);
-      cs[t * half + f] = make_float2(c * a.rope_scale, s * a.rope_scale);
+      sincospif((float)(int32_t)(at >> 32) * 0x1p-31f, &s, &c);   // (of twice the fraction, in [-1, 1])
+      cs[t * half + f] = make_float2(c * scale, s * scale);
     }
   }
 }
