@@ -505,7 +505,9 @@ catq_status catq_aux_kv_read(const catq_kv_desc* d, const catq_kv_cache* cache,
  * h / (n_q / n_kv).
  *   q, o   bf16 [n_tokens][n_q head_dim]
  *   lse    fp32 [n_tokens][n_q], log(sum_j exp(scale * q . k_j)) (NULL: not written)
- * A row that sees nothing gives o = 0 and lse = -inf.  Products are taken on fp16
+ * A row that sees nothing gives o = 0 and lse = -inf; one that sees a token is NaN if its
+ * query holds a NaN or an infinity, or if scale times its largest magnitude passes fp32.
+ * Products are taken on fp16
  * operands (the codes are exact in them; q is scaled to its row's largest
  * magnitude, and elements more than 2^14 below that lose bits; the probabilities
  * round to 11 bits), sums and softmax statistics in fp32.  A v_scale

@@ -91,6 +91,8 @@ __device__ __forceinline__ f16x8 codes8(unsigned int w0, unsigned int w1) {
 __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
+// the larger, or NaN if either is
+__device__ __forceinline__ float nan_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 // over the four lanes that hold a query's tokens
 __device__ __forceinline__ float col_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, 64));
@@ -133,10 +135,13 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
   const int c1 = min(vmax, c0 + a.span);
   const int vmin = visible(a, q, r0 / a.G);   // every row of the tile sees that much
 
-  // queries: fp16 of q over the power of two at its row's largest magnitude
+  // queries: fp16 of q over the power of two at its row's largest magnitude. A row with a NaN or an
+  // infinity in it (or a magnitude that passes fp32 times the softmax scale) is taken as zeros and made
+  // NaN at the end if it has seen a token.
   f16x8 qf[NR][2 * HH];
   float qc[NR];        // that power times the softmax scale, in log2 units
   int vis[NR];
+  bool odd[NR];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     const int row = min(r0 + 16 * r + lm, rows - 1);
@@ -150,15 +155,24 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
       float t[8];
       load8<bf16>(qp + 64 * hh, t);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { v[hh][j] = t[j]; m = fmaxf(m, fabsf(t[j])); }
+      for (int j = 0; j < 8; ++j) { v[hh][j] = t[j]; m = nan_max(m, fabsf(t[j])); }
       load8<bf16>(qp + 64 * hh + 8, t);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { v[hh][8 + j] = t[j]; m = fmaxf(m, fabsf(t[j])); }
+      for (int j = 0; j < 8; ++j) { v[hh][8 + j] = t[j]; m = nan_max(m, fabsf(t[j])); }
     }
-    m = col_max(m);
+    m = nan_max(m, __shfl_xor(m, 16, 64));
+    m = nan_max(m, __shfl_xor(m, 32, 64));
     const int e = min(max((int)(__float_as_uint(m) >> 23) - 127, -100), 126);
     const float down = __uint_as_float((unsigned)(127 - e) << 23);
     qc[r] = __uint_as_float((unsigned)(127 + e) << 23) * a.c;
+    odd[r] = !(m < INFINITY) || !(qc[r] < INFINITY);
+    if (odd[r]) {
+      qc[r] = 0.f;
+#pragma unroll
+      for (int hh = 0; hh < HH; ++hh)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[hh][j] = 0.f;
+    }
 #pragma unroll
     for (int hh = 0; hh < HH; ++hh)
 #pragma unroll
@@ -320,7 +334,8 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     if (r0 + 16 * r >= rows) break;
-    const float lr = col_sum(l[r]);
+    float lr = col_sum(l[r]);
+    if (odd[r] && lr != 0.f) lr = __builtin_nanf("");
     if (lg == 0) {
       s_m[wave][lm] = m[r];
       s_l[wave][lm] = lr;
@@ -435,9 +450,11 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
   const int wmin = visible(a, q, min(w0, rows - 1) / a.G);
   const int wmax = has_rows ? visible(a, q, min(w0 + 31, rows - 1) / a.G) : 0;
 
-  // queries: fp16 of q over the power of two at its row's largest magnitude
+  // queries as above; the score of a token on a missing page is then -inf whatever the query is.
+  // (Setting those scores in the loop took 396 us for the prompt chunks above where this takes 386.)
   f16x8 qf[KS];
   float qc;
+  bool odd;
   {
     const bf16* qp = a.Q + ((q.row0 + qi) * g.n_q + hq) * D + 8 * hh;
     float m = 0.f;
@@ -446,12 +463,18 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
     for (int k = 0; k < KS; ++k) {
       raw[k] = *reinterpret_cast<const u32x4*>(qp + 16 * k);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) m = fmaxf(m, fmaxf(fabsf(bf16_lo(raw[k][j])), fabsf(bf16_hi(raw[k][j]))));
+      for (int j = 0; j < 4; ++j) m = nan_max(m, nan_max(fabsf(bf16_lo(raw[k][j])), fabsf(bf16_hi(raw[k][j]))));
     }
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    m = nan_max(m, __shfl_xor(m, 32, 64));
     const int e = min(max((int)(__float_as_uint(m) >> 23) - 127, -100), 126);
     const float down = __uint_as_float((unsigned)(127 - e) << 23);
     qc = __uint_as_float((unsigned)(127 + e) << 23) * a.c;
+    odd = !(m < INFINITY) || !(qc < INFINITY);
+    if (odd) {
+      qc = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) raw[k] = u32x4{0u, 0u, 0u, 0u};
+    }
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -675,7 +698,8 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
             0, 0);
   }
   if (!has_rows || w0 + l32 >= rows) return;
-  const float L = l + __shfl_xor(l, 32, 64);
+  float L = l + __shfl_xor(l, 32, 64);
+  if (odd && L != 0.f) L = __builtin_nanf("");
   const int64_t at = (q.row0 + qi) * g.n_q + hq;
   // register 4 qd + e of block d: value 32 d + 8 qd + 4 hh + e
   if (a.spans > 1) {

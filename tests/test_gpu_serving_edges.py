@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_serving import BF, F64, Serving, _rand
+from test_gpu_serving import BF, F64, Serving, _attention_check, _rand
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,52 @@ def test_non_finite_frequencies(catq):
     bad = torch.zeros(d, dtype=torch.bool)
     bad[[5, 9, 37, 41]] = True
     assert torch.equal(torch.isnan(q.cpu()), bad.expand(4, d))
+
+
+# ------------------------------------------------------------------ rows and tokens that are not seen
+
+def _attend(catq, sv, q, scale=None):
+    ws = torch.empty(max(1, catq.catq_paged_attention_workspace_bytes(sv.desc, sv.batch)), dtype=torch.uint8,
+                     device="cuda")
+    o = torch.full((sv.tokens, sv.n_q * sv.d), 3.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((sv.tokens, sv.n_q), 3.0, device="cuda")
+    catq.catq_aux_paged_attention(sv.desc, sv.cache, sv.batch, q, o, ws, lse=lse, scale=scale)
+    return o, lse
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), 3e38])
+@pytest.mark.parametrize("ctx,new,ps,d", [(40, 1, 16, 64), (40, 12, 64, 128), (700, 12, 64, 64), (40, 40, 16, 128),
+                                          (40, 40, 64, 64), (3000, 40, 128, 128), (40, 200, 32, 64), (40, 200, 64, 128),
+                                          (40, 40, 64, 256)])
+def test_a_row_that_sees_nothing_is_zero(catq, ctx, new, ps, d, value):
+    """Also where its query is not finite, or so large that its scores are not."""
+    sv = Serving(catq, [(ctx, new), (33, new)], 2, 1, d, ps, 16)
+    sv.table[0] = -1
+    sv.upload()
+    q = _rand(sv.g, sv.tokens, 2 * d)
+    clean = q.clone()
+    q[:new] = value
+    o, lse = _attend(catq, sv, q.cuda(), scale=200.0 if value == 3e38 else None)
+    assert (o[:new] == 0).all() and torch.isneginf(lse[:new]).all()
+    if value != 3e38:
+        _attention_check(o, lse, sv, clean, sv.oracle())
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("new,d", [(1, 64), (1, 128), (12, 256), (40, 64), (40, 128), (200, 128)])
+def test_a_query_that_is_not_finite_gives_nan(catq, new, d, value):
+    """One such value is enough, also where every score it makes is -infinite, and in no other row."""
+    sv = Serving(catq, [(0, new), (600, new)], 2, 1, d, 64, 16)
+    sv.k[:] = -sv.k.abs() - (sv.k == 0).to(torch.int8)          # (no code is 0)
+    sv.upload()
+    q = _rand(sv.g, sv.tokens, 2 * d)
+    bad = torch.zeros((sv.tokens, 2), dtype=torch.bool)
+    bad[[0, sv.tokens - 1], [1, 0]] = True
+    p = q.clone()
+    p[0, d + 3] = p[-1, d - 1] = value
+    (o, lse), (clean, cl) = _attend(catq, sv, p.cuda()), _attend(catq, sv, q.cuda())
+    rows = o.view(-1, 2, d)
+    assert torch.isnan(rows[bad.cuda()]).all() and torch.equal(torch.isnan(lse.cpu()), bad)
+    rows[bad.cuda()] = clean.view(-1, 2, d)[bad.cuda()]
+    lse[bad.cuda()] = cl[bad.cuda()]
+    _attention_check(o, lse, sv, q, sv.oracle())
