@@ -21,9 +21,9 @@
 // Scales: a k scale multiplies the scores, with the softmax scale and the row's q scale. A v
 // scale moves into the exponent, p' = 2^(s + log2 v_scale - m), which keeps p' within 2^8
 // whatever the scales are (fp16 operands); the denominator adds p' / v_scale.  p' underflows
-// at 2^-126, so a token is lost from the denominator where its scale is 2^90 below the
-// scale behind the maximum and its weight is not yet under 2^-36: scales are
-// therefore held to [2^-60, 2^30], where that cannot be.
+// at 2^-126, so a token is lost from the denominator where its scale is 2^91 below the
+// scale behind the maximum and its weight is not yet under 2^-35: scales are
+// therefore held to [2^-61, 2^30], where that cannot be.
 // The running maximum is only raised when a score exceeds it by 2^8 (p' <= 256 is as good
 // in fp16 as p' <= 1), so the rescaling of the output is rare.
 //
@@ -414,8 +414,10 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
 // waves of a SIMD turns (one multiplies, one exponentiates, a barrier between) brought nothing
 // (420 us), nor did half tiles interleaved inside a wave (they spill).
 // A tile's v scale is in lv (log2, NaN outside its range, -inf on a page that does not
-// exist) and rv (its reciprocal, always finite, so that a masked token adds 0).
+// exist) and rv (its reciprocal, always finite, so that a masked token adds 0). One that counts as 0
+// has the lv and rv of 2^-61, which no scale that counts has.
 constexpr int kTile = 64, kPitch = kTile + 1;
+constexpr float kTinyLog = -61.0f;
 
 template <int D, int NW, bool PER_TOKEN>
 __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
@@ -576,8 +578,8 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
     if (wave == 0) {
       const bool tiny = vsr < kTinyScale, fine = vsr <= kHugeScale && !tiny;
       s_ks[buf][lane] = none ? 0.f : ksr;
-      s_lv[buf][lane] = none ? -INFINITY : fine ? __builtin_amdgcn_logf(vsr) : tiny ? -60.f : __builtin_nanf("");
-      s_rv[buf][lane] = none || !(fine || tiny) ? 1.f : __builtin_amdgcn_rcpf(fine ? vsr : kTinyScale);
+      s_lv[buf][lane] = none ? -INFINITY : fine ? __builtin_amdgcn_logf(vsr) : tiny ? kTinyLog : __builtin_nanf("");
+      s_rv[buf][lane] = none || !(fine || tiny) ? 1.f : __builtin_amdgcn_rcpf(fine ? vsr : 0.5f * kTinyScale);
       s_tiny[buf] = __any(tiny && !none);
     }
   };
@@ -687,7 +689,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (s_lv[buf][32 * u + 8 * (i >> 2) + 4 * hh + (i & 3)] == -60.f) p[u][i >> 3][i & 7] = (f16)0.f;
+          if (s_lv[buf][32 * u + 8 * (i >> 2) + 4 * hh + (i & 3)] == kTinyLog) p[u][i >> 3][i & 7] = (f16)0.f;
     }
 #pragma unroll
     for (int T = 0; T < 4; ++T)

@@ -127,3 +127,20 @@ def test_a_query_that_is_not_finite_gives_nan(catq, new, d, value):
     rows[bad.cuda()] = clean.view(-1, 2, d)[bad.cuda()]
     lse[bad.cuda()] = cl[bad.cuda()]
     _attention_check(o, lse, sv, q, sv.oracle())
+
+
+@pytest.mark.parametrize("bt", [1, 16])
+@pytest.mark.parametrize("new", [1, 12, 40, 300])
+def test_attention_scales_at_the_border(catq, new, bt):
+    """A v scale of 2^-60, or one step above, counts, beside others that are below and do not."""
+    sv = Serving(catq, [(90, new), (33, new)], 2, 1, 128, 64, bt)
+    low = torch.rand(sv.vs.shape, generator=sv.g)
+    sv.vs[:] = 2.0 ** -60
+    sv.vs[low < 0.6] = 2.0 ** -60 * (1 + 2.0 ** -23)
+    sv.vs[low < 0.3] = 2.0 ** -60 * (1 - 2.0 ** -24)
+    sv.upload()
+    q = _rand(sv.g, sv.tokens, 256)
+    o, lse = _attend(catq, sv, q.cuda())
+    oracle = sv.oracle()
+    oracle.scales[1][oracle.scales[1] < 2.0 ** -60] = 0
+    _attention_check(o, lse, sv, q, oracle)
