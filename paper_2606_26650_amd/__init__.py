@@ -323,6 +323,15 @@ def _act(t, name):
     return dt
 
 
+def _per_group(t, name, rows, n, group, device):
+    """t, fp32 [rows][n/group] (the rows in any number of dimensions, or all of it flat)."""
+    _want(t, name, torch.float32, None, device)
+    if group > 0:     # (the library refuses the others)
+        each = n // group
+        if t.numel() != rows * each or (each > 1 and t.dim() != 1 and t.shape[-1] != each):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(rows, each)}")
+
+
 def _rows(t, name, shape, device):
     """The row stride of a 2-d tensor whose rows are contiguous."""
     if t.shape != shape:
@@ -338,6 +347,8 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 
 
 def _run_on(device, stream, fn, name, *args):
+    if device < 0:
+        raise ValueError(f"{name}: the tensors must be on a GPU")
     if device == _current_device():
         st = fn(*args, _stream(stream) if _raw_stream is None or stream is not None else _raw_stream(device))
     else:
@@ -357,8 +368,8 @@ def catq_aux_rmsnorm_quant(x, q=None, scale=None, res=None, weight=None, sum=Non
     with their scales [rows][n/group] (default: one per row), or their values y in
     bf16, or both."""
     xd = _act(x, "x")
-    _want(x, "x", x.dtype)
     shape, dev = x.shape, x.get_device()
+    _want(x, "x", x.dtype, None, dev)
     n = shape[-1]
     rows = x.numel() // n if n else 0
     if group is None:
@@ -378,9 +389,7 @@ def catq_aux_rmsnorm_quant(x, q=None, scale=None, res=None, weight=None, sum=Non
     if q is not None:
         _want(q, "q", torch.int8, shape, dev)
     if scale is not None:
-        _want(scale, "scale", torch.float32, None, dev)
-        if group > 0 and scale.numel() != rows * (n // group):
-            raise ValueError(f"scale: {scale.numel()} values, expected {rows * (n // group)}")
+        _per_group(scale, "scale", rows, n, group, dev)
     _run_on(dev, stream, lib.catq_aux_rmsnorm_quant, "catq_aux_rmsnorm_quant", x.data_ptr(), xd, _ptr(res), rd,
             _ptr(weight), rows, n, group, eps, _ptr(sum), _ptr(y), _ptr(q), _ptr(scale))
 
@@ -389,15 +398,13 @@ def catq_aux_act_quant8(x, q, scale, group=None, stream=None):
     """The 8-bit codes of every group of ``group`` consecutive values of x's rows
     (default: the whole row) and their scales."""
     xd = _act(x, "x")
-    _want(x, "x", x.dtype)
     n, dev = x.shape[-1], x.get_device()
+    _want(x, "x", x.dtype, None, dev)
     rows = x.numel() // n if n else 0
     if group is None:
         group = n
     _want(q, "q", torch.int8, x.shape, dev)
-    _want(scale, "scale", torch.float32, None, dev)
-    if group > 0 and scale.numel() != rows * (n // group):
-        raise ValueError(f"scale: {scale.numel()} values, expected {rows * (n // group)}")
+    _per_group(scale, "scale", rows, n, group, dev)
     _run_on(dev, stream, lib.catq_aux_act_quant8, "catq_aux_act_quant8", x.data_ptr(), xd, rows, n, group,
             q.data_ptr(), scale.data_ptr())
 
@@ -406,8 +413,8 @@ def catq_ternary_linear_a8(q, x_scale, packed, alpha, Y, g=128, stream=None):
     """Y = x_scale * q (alpha * T)^T from the 2-bit storage: codes q int8 [M][d_in]
     (rows may be strided), x_scale fp32 [M], packed uint8 [d_out][d_in/4], alpha
     fp32 [d_out][d_in/g], Y fp32 or bf16 [M][d_out] (rows may be strided)."""
-    _want(packed, "packed", torch.uint8)
     dev = packed.get_device()
+    _want(packed, "packed", torch.uint8, None, dev)
     d_out, d_in = packed.shape[0], packed.shape[1] * 4
     M = q.shape[0]
     if q.dtype is not torch.int8:
@@ -415,11 +422,9 @@ def catq_ternary_linear_a8(q, x_scale, packed, alpha, Y, g=128, stream=None):
     yd = _act(Y, "Y")
     ldq, ldy = _rows(q, "q", (M, d_in), dev), _rows(Y, "Y", (M, d_out), dev)
     _want(x_scale, "x_scale", torch.float32, None, dev)
-    _want(alpha, "alpha", torch.float32, None, dev)
     if x_scale.numel() != M:
         raise ValueError(f"x_scale: {x_scale.numel()} values, expected {M}")
-    if g > 0 and alpha.numel() != d_out * (d_in // g):
-        raise ValueError(f"alpha: {alpha.numel()} values, expected {d_out * (d_in // g)}")
+    _per_group(alpha, "alpha", d_out, d_in, g, dev)
     _run_on(dev, stream, lib.catq_ternary_linear_a8, "catq_ternary_linear_a8", q.data_ptr(), M, ldq,
             x_scale.data_ptr(), packed.data_ptr(), alpha.data_ptr(), d_out, d_in, g, Y.data_ptr(), yd, ldy)
 

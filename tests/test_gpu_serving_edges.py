@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_serving import BF, F64, Serving, _attention_check, _rand
+from test_gpu_serving import BF, F64, Serving, _attention_check, _linear_inputs, _rand
 
 pytestmark = pytest.mark.gpu
 
@@ -144,3 +144,20 @@ def test_attention_scales_at_the_border(catq, new, bt):
     oracle = sv.oracle()
     oracle.scales[1][oracle.scales[1] < 2.0 ** -60] = 0
     _attention_check(o, lse, sv, q, oracle)
+
+
+# ------------------------------------------------------------------ arguments in another order
+
+def test_scales_in_another_order_are_refused(catq):
+    """alpha and scales laid out group by group are not read as rows of groups; nothing is written."""
+    q, packed, alpha, xs = [t.cuda() for t in _linear_inputs(5, 24, 512, 128, 0)]
+    Y = torch.full((5, 24), 5.0, device="cuda")
+    with pytest.raises(ValueError, match="alpha"):
+        catq.catq_ternary_linear_a8(q, xs, packed, alpha.T.contiguous(), Y)
+    x = torch.ones((5, 512), dtype=torch.bfloat16, device="cuda")
+    s = torch.full((4, 5), 5.0, device="cuda")
+    with pytest.raises(ValueError, match="scale"):
+        catq.catq_aux_act_quant8(x, q, s, group=128)
+    with pytest.raises(ValueError, match="scale"):
+        catq.catq_aux_rmsnorm_quant(x, q, s, group=128)
+    assert (Y == 5.0).all() and (s == 5.0).all()

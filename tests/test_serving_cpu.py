@@ -195,6 +195,30 @@ def test_python_checks(cq):
         cq.kv_prep(d, torch.zeros(32, dtype=torch.float64), rot_dim=64)
 
 
+def test_scales_in_another_order_are_refused(cq):
+    """Scales and alpha laid out group by group have the right count; flat ones, and rows in several
+    dimensions, are taken (up to the refusal of host tensors)."""
+    z = torch.zeros
+    x, q = z(6, 512, dtype=torch.bfloat16), z(6, 512, dtype=torch.int8)
+    packed, Y = z(24, 128, dtype=torch.uint8), z(6, 24)
+    norm = lambda s, **kw: cq.catq_aux_rmsnorm_quant(x, q, s, **kw)                     # noqa: E731
+    quant = lambda s, **kw: cq.catq_aux_act_quant8(x, q, s, **kw)                       # noqa: E731
+    linear = lambda a, **kw: cq.catq_ternary_linear_a8(q, z(6), packed, a, Y, **kw)     # noqa: E731
+    for call in (lambda: norm(z(4, 6), group=128), lambda: quant(z(4, 6), group=128), lambda: linear(z(4, 24)),
+                 lambda: linear(z(24, 2, 2)), lambda: linear(z(2, 24), g=256), lambda: norm(z(6, 3), group=128),
+                 lambda: norm(z(4, 6).T, group=128), lambda: linear(z(24, 8)[:, ::2])):
+        with pytest.raises(ValueError, match="scale|alpha"):
+            call()
+    for call in (lambda: norm(z(6, 4), group=128), lambda: norm(z(24), group=128), lambda: norm(z(2, 3, 4), group=128),
+                 lambda: norm(z(6)), lambda: norm(z(6, 1)), lambda: norm(z(1, 6)), lambda: quant(z(6, 4), group=128),
+                 lambda: linear(z(24, 4)), lambda: linear(z(96)), lambda: linear(z(1, 24), g=512),
+                 lambda: linear(z(24, 4), g=128)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    with pytest.raises(ValueError, match="GPU"):
+        cq.catq_ternary_linear_a8(q[:0], z(0), packed, z(24, 4), Y[:0])
+
+
 # ---------------------------------------------------------------- the reference itself
 
 def test_reference_rotation():
