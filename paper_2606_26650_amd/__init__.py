@@ -429,8 +429,17 @@ def catq_ternary_linear_a8(q, x_scale, packed, alpha, Y, g=128, stream=None):
             x_scale.data_ptr(), packed.data_ptr(), alpha.data_ptr(), d_out, d_in, g, Y.data_ptr(), yd, ldy)
 
 
+def _int32(**sizes):
+    """Sizes that a descriptor holds in 32 bits (a ctypes field would drop the upper ones)."""
+    for name, v in sizes.items():
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{name}: {v} does not fit 32 bits")
+
+
 def kv_desc(n_q, n_kv, head_dim, page_size, scale_block, n_pages, max_pages):
     """Geometry of a paged 8-bit cache (see catq_kv_desc in the header)."""
+    _int32(n_q=n_q, n_kv=n_kv, head_dim=head_dim, page_size=page_size, scale_block=scale_block, n_pages=n_pages,
+           max_pages=max_pages)
     return KvDesc(n_q, n_kv, head_dim, page_size, scale_block, n_pages, max_pages)
 
 
@@ -455,6 +464,7 @@ def kv_batch(desc, page_table, cu_new, ctx_len, n_tokens, max_new, max_len):
     [n_seqs][max_pages], cu_new int32 [n_seqs + 1], ctx_len int32 [n_seqs], on the
     device; their values may change between calls.  The returned struct keeps them."""
     n = ctx_len.shape[0]
+    _int32(max_new=max_new, max_len=max_len)
     _want(page_table, "page_table", torch.int32, (n, desc.max_pages))
     dev = page_table.get_device()
     _want(cu_new, "cu_new", torch.int32, (n + 1,), dev)
@@ -468,6 +478,7 @@ def kv_prep(desc, inv_freq=None, rot_dim=0, interleaved=False, qk_norm=False, q_
             eps=1e-6, rope_scale=1.0, act_quant=False):
     """What happens to q and k on the way to the cache (see catq_kv_prep in the
     header).  The returned struct keeps the tensors."""
+    _int32(rot_dim=rot_dim)
     first = next((t for t in (inv_freq, q_weight, k_weight) if t is not None), None)
     dev = None if first is None else first.get_device()
     if inv_freq is not None:

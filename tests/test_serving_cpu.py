@@ -219,6 +219,24 @@ def test_scales_in_another_order_are_refused(cq):
         cq.catq_ternary_linear_a8(q[:0], z(0), packed, z(24, 4), Y[:0])
 
 
+def test_sizes_past_32_bits_are_refused(cq):
+    """Not cut to their lower 32 bits, which would be another size."""
+    ok = dict(n_q=4, n_kv=2, head_dim=64, page_size=16, scale_block=16, n_pages=3, max_pages=2)
+    for name in ok:
+        for far in (2 ** 32, -2 ** 32, 2 ** 31):
+            with pytest.raises(ValueError, match=name):
+                cq.kv_desc(**dict(ok, **{name: ok[name] + far}))
+    d = cq.kv_desc(**ok)
+    arrays = [torch.zeros(s, dtype=torch.int32) for s in ((1, 2), (2,), (1,))]
+    with pytest.raises(ValueError, match="max_new"):
+        cq.kv_batch(d, *arrays, 5, 2 ** 32 + 1, 20)
+    with pytest.raises(ValueError, match="max_len"):
+        cq.kv_batch(d, *arrays, 5, 1, 2 ** 32 + 20)
+    with pytest.raises(ValueError, match="rot_dim"):
+        cq.kv_prep(d, rot_dim=2 ** 32)
+    assert cq.kv_desc(**dict(ok, n_pages=2 ** 31 - 1)).n_pages == 2 ** 31 - 1
+
+
 # ---------------------------------------------------------------- the reference itself
 
 def test_reference_rotation():
