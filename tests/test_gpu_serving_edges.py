@@ -1,4 +1,6 @@
-"""Calls of the serving operators at the ends of their ranges."""
+"""Calls of the serving operators at the ends of their ranges: far positions and large frequencies,
+pages that are missing, contents behind the mask, scales at the border of what counts, rows that
+see nothing, storage at its least alignment."""
 import math
 from fractions import Fraction
 
@@ -6,7 +8,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_serving import BF, F64, Serving, _attention_check, _linear_inputs, _rand
+import serving_ref as ref
+from test_gpu_serving import BF, F64, Serving, _attention_check, _linear_check, _linear_inputs, _rand
 
 pytestmark = pytest.mark.gpu
 
@@ -161,3 +164,119 @@ def test_scales_in_another_order_are_refused(catq):
     with pytest.raises(ValueError, match="scale"):
         catq.catq_aux_rmsnorm_quant(x, q, s, group=128)
     assert (Y == 5.0).all() and (s == 5.0).all()
+
+
+MASKED = [(20, 1), (20, 10), (35, 30), (20, 200), (1500, 1), (1500, 10), (1500, 40)]   # ctx, new: one span and several
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("bt", [1, 16])
+@pytest.mark.parametrize("ctx,new", MASKED)
+def test_attention_contents_behind_the_mask(catq, ctx, new, bt, d):
+    """NaN and infinite scales at positions that a row does not see, in its own pages and in others', change
+    nothing in it; the rows that see one are NaN."""
+    sv = Serving(catq, [(ctx, new)], 2, 1, d, 64, bt, extra_pages=2)
+    total, q = ctx + new, _rand(sv.g, new, 2 * d)
+    oracle = sv.oracle()
+    pages = sv.table[0, :-(-total // 64)]
+    other = [p for p in range(sv.desc.n_pages) if p not in pages.tolist()]
+    tail = -(-(total % 64) // bt)                 # first block of the last page that no row sees
+    assert other and total % 64 and tail < 64 // bt
+    for s, a, b in ((sv.ks, math.nan, math.inf), (sv.vs, math.inf, math.nan)):
+        s[other] = a
+        s[pages[-1], :, tail:] = b
+    sv.upload()
+    o, lse = _attend(catq, sv, q.cuda())
+    _attention_check(o, lse, sv, q, oracle)
+    # a block that the later rows see, in k and then in v
+    start = -(-(ctx + new // 2) // bt) * bt
+    if start >= total:
+        return
+    first = max(0, start - ctx)
+    for w in (2, 3):
+        held = sv.dev[w].clone()
+        sv.dev[w][pages[start // 64], :, start % 64 // bt] = math.nan
+        got, gl = _attend(catq, sv, q.cuda())
+        sv.dev[w].copy_(held)
+        assert torch.isnan(got[first:]).all() and torch.isnan(gl[first:]).all()
+        got[first:], gl[first:] = o[first:], lse[first:]
+        _attention_check(got, gl, sv, q, oracle)
+
+
+@pytest.mark.parametrize("ctx,new,d", [(100, 1, 64), (100, 14, 128), (100, 40, 64), (100, 200, 128), (1500, 1, 128),
+                                       (1500, 14, 64), (1500, 40, 128), (1500, 300, 64), (900, 30, 256)])
+@pytest.mark.parametrize("ps,bt", [(16, 16), (16, 1), (32, 16), (64, 64), (128, 1)])
+def test_attention_over_missing_pages(catq, ctx, new, d, ps, bt):
+    """Page ids that are none, first, last, single and several in a row between the others: their tokens are
+    unseen, whatever page 0 holds."""
+    sv = Serving(catq, [(ctx, new), (37, 2)], 2, 1, d, ps, bt)
+    n = -(-(ctx + new) // ps)
+    gone = torch.rand(n, generator=sv.g) < 0.3
+    gone[n // 2] = True
+    gone[n // 3] = False
+    sv.table[0, :n][gone] = torch.tensor([-1, -2 ** 31, sv.desc.n_pages, 2 ** 31 - 1], dtype=torch.int32)[
+        torch.randint(0, 4, (int(gone.sum()),), generator=sv.g)]
+    if 0 not in sv.table.tolist()[0] + sv.table.tolist()[1]:
+        sv.ks[0], sv.vs[0] = math.nan, math.nan
+    sv.upload()
+    q = _rand(sv.g, sv.tokens, 2 * d)
+    o, lse = _attend(catq, sv, q.cuda())
+    _attention_check(o, lse, sv, q, sv.oracle())
+
+
+@pytest.mark.parametrize("bt", [1, 16, 64])
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_beside_scales_past_the_range(catq, bt, new):
+    """V scales from 1e-20 to 1e12: where a row sees none above 2^30 it is as the reference has it, with the
+    scales below 2^-60 counted as 0."""
+    sv = Serving(catq, [(200, new), (70, new)], 4, 2, 128, 64, bt)
+    g = sv.g
+    sv.vs *= 10.0 ** (torch.rand(sv.vs.shape, generator=g) * 26 - 20)
+    held = sv.table[1, :-(-(70 + new) // 64)].long()
+    sv.vs[held, 0] = sv.vs[held, 0].clamp(max=2.0 ** 30)         # one sequence's one head sees none
+    sv.vs[sv.table[0, 0], 0, 0] = 2.0 ** 31                      # another sequence's first block is
+    sv.upload()
+    q = _rand(g, sv.tokens, 4 * 128)
+    o, lse = _attend(catq, sv, q.cuda())
+    oracle = sv.oracle()
+    oracle.scales[1][oracle.scales[1] < 2.0 ** -60] = 0
+    seen = torch.zeros((sv.tokens, 2), dtype=F64)      # the largest scale that each row's heads see
+    for i, (ctx, n) in enumerate(sv.seqs):
+        for r in range(n):
+            top = torch.stack([oracle.scales[1][(at := oracle.place(sv.table[i], p))[0], :, at[1] // bt]
+                               for p in range(ctx + r + 1)]).amax(0)
+            seen[int(sv.cu[i]) + r] = top
+    bad = (seen > 2.0 ** 30).repeat_interleave(2, 1)
+    assert bad.any() and (~bad).any()
+    assert torch.equal(torch.isnan(lse.cpu()), bad)
+    rows = o.view(-1, 4, 128)
+    assert torch.isnan(rows[bad.cuda()]).all() and torch.isfinite(rows[~bad.cuda()].float()).all()
+    # the rows that are not NaN, against the reference (its own values in the others' place)
+    for i, (ctx, n) in enumerate(sv.seqs):
+        r0 = int(sv.cu[i])
+        w, wl = ref.attention(q[r0:r0 + n].to(F64).view(n, 4, 128), oracle, sv.table[i], ctx, 128 ** -0.5, 2)[:2]
+        b = bad[r0:r0 + n].cuda()
+        rows[r0:r0 + n][b] = w.bfloat16().cuda()[b]
+        lse[r0:r0 + n][b] = wl.float().cuda()[b]
+    _attention_check(o, lse, sv, q, oracle)
+
+
+# ------------------------------------------------------------------ the product's storage
+
+@pytest.mark.parametrize("M,d_out,d_in,g", [(1, 100, 640, 128), (4, 4111, 2176, 128), (16, 333, 1024, 512),
+                                            (33, 34001, 896, 128), (45, 16421, 2176, 128), (48, 5120, 1152, 128),
+                                            (130, 515, 1280, 128), (1000, 16421, 128, 128), (257, 300, 896, 128)])
+def test_linear_a8_storage_at_its_least_alignment(catq, M, d_out, d_in, g):
+    """packed 8 bytes past a multiple of 16, x_scale and a bf16 Y 4 bytes past one."""
+    q, packed, alpha, xs = _linear_inputs(M, d_out, d_in, g, M + d_in)
+    held = torch.full((packed.numel() + 16,), 0xFF, dtype=torch.uint8, device="cuda")
+    dp = held[8:8 + packed.numel()].view(packed.shape)
+    dp.copy_(packed)
+    dx = torch.full((M + 2,), float("nan"), device="cuda")[1:M + 1]
+    dx.copy_(xs)
+    room = torch.full((M * d_out + 4,), 5.0, dtype=torch.bfloat16, device="cuda")
+    Y = room[2:2 + M * d_out].view(M, d_out)
+    assert dp.data_ptr() % 16 == 8 and dx.data_ptr() % 16 == 4 and Y.data_ptr() % 16 == 4
+    catq.catq_ternary_linear_a8(q.cuda(), dx, dp, alpha.cuda(), Y, g=g)
+    _linear_check(Y, q, packed, alpha, xs, g, True)
+    assert (room[:2] == 5.0).all() and (room[2 + M * d_out:] == 5.0).all()
