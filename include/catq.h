@@ -372,7 +372,9 @@ catq_status catq_aux_act_quant(const void* x, catq_dtype x_dtype, int64_t rows, 
  *   +-127 (0 where scale = 0), y = bf16(q * scale)
  * all in IEEE fp32.  A group that holds a NaN or an infinity gets a NaN scale
  * and zero codes.  catq_aux_act_quant8 has no norm, residual or weight (xh = x):
- * its codes stand for exactly the values of catq_aux_act_quant on finite x.
+ * its codes stand for exactly the values of catq_aux_act_quant on finite x.  (With the
+ * norm they are of unrounded values, where the calibration's forward quantizes the
+ * stored bf16 ones: a value near a half can take the next code.)
  *   x       [rows][n] of x_dtype; res, sum [rows][n] of r_dtype (both NULL, or
  *           res given and sum NULL or not); sum may be res, or x where the types agree
  *   y       bf16 [rows][n], may be NULL;  q int8 [rows][n] and scale fp32
@@ -486,7 +488,9 @@ typedef struct {
  * round-half-even(code * (old scale / new scale)) where the scale grows.  A block
  * that receives a NaN or an infinity gets a NaN scale.  A block that receives tokens
  * belongs to one sequence of the batch; pages can be shared otherwise.  Appending
- * the same tokens again gives the same cache.
+ * the same tokens again gives the same cache.  A scale_block of 1 is what the
+ * calibration simulates (a scale per token and head); larger ones take less memory and
+ * lose accuracy, more where they are filled token by token.
  * catq_aux_kv_read: positions ctx_len[s] + i back as the bf16 values they stand for,
  * k_out and v_out [n_tokens][n_kv head_dim] (either may be NULL).
  * Every pointer 16-byte aligned.
@@ -514,7 +518,9 @@ catq_status catq_aux_kv_read(const catq_kv_desc* d, const catq_kv_cache* cache,
  * below 2^-60 counts as 0, and one above 2^30 as NaN: rows that see it are NaN.  The context is split over workgroups where few rows
  * are asked for; the workspace then holds their partial results: at least
  * catq_paged_attention_workspace_bytes(d, batch) bytes (0: may be NULL), for one call at a
- * time.  Deterministic for given sizes (n_seqs, n_tokens, max_new, max_len).
+ * time.  Deterministic for given sizes (n_seqs, n_tokens, max_new, max_len).  The split is
+ * one for the whole batch: sequences far longer than the others, and prompt chunks beside
+ * single tokens, are faster in calls of their own.
  */
 size_t catq_paged_attention_workspace_bytes(const catq_kv_desc* d, const catq_kv_batch* batch);
 catq_status catq_aux_paged_attention(const catq_kv_desc* d, const catq_kv_cache* cache,

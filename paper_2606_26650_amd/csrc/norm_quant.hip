@@ -130,7 +130,7 @@ __global__ __launch_bounds__(NT) void norm_quant_kernel(NormQuantArgs a) {
     for (int k = cpg >> 1; k >= 1; k >>= 1)
 #pragma unroll
       for (int i = 0; i < CH; ++i) mag[i] = max(mag[i], (unsigned)__shfl_xor((int)mag[i], k, 64));
-  } else {
+  } else {   // (any other group: one value after the other, as many as a group has chunks)
 #pragma unroll
     for (int i = 0; i < CH; ++i) s_mag[tid + NT * i] = mag[i];
     __syncthreads();

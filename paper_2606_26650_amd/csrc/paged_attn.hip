@@ -24,6 +24,11 @@
 // at 2^-126, so a token is lost from the denominator where its scale is 2^91 below the
 // scale behind the maximum and its weight is not yet under 2^-35: scales are
 // therefore held to [2^-61, 2^30], where that cannot be.
+// p' is rounded to fp16 for the second product, 2^-11 of each term and an eighth of the half step that the
+// bf16 output loses (the sum l adds it in fp32, unrounded); a second product for its lower bits would be
+// half as many again. exp2, log2 and the reciprocal are the hardware's, off by one unit of fp32
+// each, below the d roundings of a score: the library's add instructions for denormals and the last
+// bit, which neither the output nor a score holds.
 // The running maximum is only raised when a score exceeds it by 2^8 (p' <= 256 is as good
 // in fp16 as p' <= 1), so the rescaling of the output is rare.
 //
@@ -809,7 +814,12 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
 
 // How a call is split: rows per workgroup (16 or 32: the waves split the context; 128 or 256: the
 // waves split the rows; 256 rows share a tile's conversion, 404 us for three prompt chunks where
-// 128 take 421) and spans of the context.
+// 128 take 421) and spans of the context. Both are chosen once for the batch, from max_new and
+// max_len: one sequence of 131072 tokens among 63 of 500 is walked in one span (1391 us; 50 and 17
+// in calls of their own), and 63 single tokens after 4000 beside a chunk of 2000 take its tiles
+// (904 us; 94 and 81). Heads of 256 have tiles of at most 32 rows: 256 values a row do not fit the
+// registers of the other kernel, and those of this one spill 13-18 (1000 tokens after 1000, 16 + 4
+// heads: 105 us, where a kernel at the rate of the products would take 17).
 struct Plan {
   int tile_rows, row_tiles, spans, span;
 };

@@ -280,11 +280,11 @@ __global__ __launch_bounds__(NW * 64) void ternary_a8_gemv_kernel(A8Args a) {
 // chunk's values 64 h .. 64 h + 63, in four contraction steps of v_mfma_i32_32x32x32_i8.  The sums of
 // a chunk are converted and added with the rows' scales; with larger groups only once a group.
 //
-// 1000 x 34816 x 5120: 275 us, 1.3 PFLOP/s, at a clock of 1.9 GHz.  What bounds it is the
-// vector instructions: 145 per wave and chunk (64 convert and scale the sums, 44 decode, 16 bring
-// activations into order, 8 with eight waves) take 72% of the issue cycles, beside matrix cores at 32% and the LDS
-// reads of the operands at half of its bandwidth, four waves per SIMD overlapping them; leaving
-// out any one of them gains 5-15%, the activations' staging 18%.
+// 1000 x 34816 x 5120 with eight waves: 275 us, 1.3 PFLOP/s, at a clock of 1.9 GHz.  What bounds it is the
+// vector instructions: 136 per wave and chunk (64 convert and scale the sums, 44 decode, 8 bring
+// activations into order; 145 with four waves, 16 of them for the order) take 65% of the issue cycles (72% with
+// four), beside matrix cores at 30% and the LDS reads of the operands at half of its bandwidth, four waves per SIMD
+// overlapping them.  With four waves, leaving out any one of them gained 5-15%, the activations' staging 18%.
 template <int NWV, int CB, bool G128, typename OutT>
 __global__ __launch_bounds__(NWV * 64, 4) void ternary_a8_gemm_kernel(A8Args a) {
   constexpr int T = NWV * 64, RT = 32 * NWV, TT = 32 * CB;
@@ -544,9 +544,11 @@ extern "C" catq_status catq_ternary_linear_a8(const int8_t* q, int64_t M, int64_
                      (double)M * (double)d_in + (double)M * (double)d_out * (double)dtype_size(y_dtype)};
   // Which kernel: the least of a cost model in microseconds, fitted on MI355X over 56 sizes (1024 x 5120
   // to 100000 x 2048, one token to 100; its choice is 3% behind the best of 15 on average, 14% at
-  // worst).  A launch costs base; then per chunk a workgroup alone on its compute unit takes alone,
-  // and several of them each apiece.  5120 x 17408: R = 1 at one token (9.1 us; 13.7 for R = 2), R = 2
-  // with three token tiles at 48 (19.9; 21.3 with one, 24.6 with two).  34816 x 5120: R = 2 on four waves at one
+  // worst).  It is fitted for the choice: the times themselves are too long where a last round of
+  // workgroups is nearly empty (5120 x 17408 at one token: 14.4, measured 9.1).  A launch costs base;
+  // then per chunk a workgroup alone on its compute unit takes alone, and several of them each
+  // apiece.  Measured with the fit, 5120 x 17408: R = 1 at one token (9.1 us; 13.7 for R = 2), R = 2
+  // with three token tiles at 48 (19.9, 18.4 as the kernel is now; 21.3 with one, 24.6 with two).  34816 x 5120: R = 2 on four waves at one
   // token (13.3; 14.4 for R = 1), R = 3 on four waves with two token tiles at 48 (32.2; tiled 38.2), tiled from 64.
   // 8192 x 8192 at 16: R = 1 (8.4; 9.9 for R = 2 with two token tiles).
   const int ng = a.n_chunks >> a.cpg_shift;
