@@ -528,6 +528,65 @@ catq_status catq_aux_paged_attention(const catq_kv_desc* d, const catq_kv_cache*
                                      void* o, float* lse, void* workspace,
                                      size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * Drafted tokens as a tree: the new tokens of a sequence need not follow each other.
+ * They take the cache slots ctx_len[s] + i as always, in any order that puts a token behind
+ * those it continues.
+ */
+typedef struct {
+  const uint64_t* mask;   /* [n_tokens][words]: bit j % 64 of word j / 64 of row r is set if the row
+                             sees new token j of its sequence (itself too only if its own
+                             bit is set).  Bits past the sequence's new tokens are ignored  */
+  const int32_t* depth;   /* [n_tokens]: the row's k and q turn by position ctx_len[s] + depth; NULL
+                             for ctx_len[s] + i                                        */
+  int32_t words;          /* at least max_new / 64 rounded up, at most 1024            */
+} catq_kv_tree;           /* mask 8-byte aligned, depth 4-byte                          */
+
+/*
+ * catq_aux_kv_append_tree: catq_aux_kv_append with each token rotated for the depth it has in
+ * the tree (mask is not read and may be NULL).
+ * catq_aux_tree_attention: catq_aux_paged_attention where row i of sequence s sees every
+ * position before ctx_len[s], and of the new tokens those that its mask names.  The depth is not
+ * read.  A row that sees nothing (an empty mask behind no cached token) gives o = 0 and lse =
+ * -inf; contents of the cache that a row does not see do not reach it, whatever they are.  Everything
+ * else, the workspace too, is as for catq_aux_paged_attention.
+ */
+catq_status catq_aux_kv_append_tree(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                    const catq_kv_batch* batch, const catq_kv_tree* tree,
+                                    const catq_kv_prep* prep, const void* qkv, void* q_out,
+                                    hipStream_t stream);
+catq_status catq_aux_tree_attention(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                    const catq_kv_batch* batch, const catq_kv_tree* tree, const void* q,
+                                    float scale, void* o, float* lse, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Pages.  A page table row is the caller's: two sequences share what they have in common by
+ * naming the same pages, and a page that no row names is free.
+ * catq_aux_kv_copy_pages: page dst[i] becomes a copy of page src[i], i = 0 .. n-1 (codes and scales;
+ *   src and dst on the device).  What a fork does with the last, partly filled page of a sequence
+ *   before it appends, and how a pool is made dense.  A pair with an id outside [0, n_pages) or with
+ *   src[i] = dst[i] is left out.  A page may be the source of several pairs; one that is a
+ *   destination may be in no other pair of the call.
+ * catq_aux_kv_compact: of the new tokens of sequence s, the n_keep[s] (int32 [n_seqs]) named by
+ *   keep[cu_new[s] + i] (int32 [n_tokens]; rising, each in 0 .. new tokens - 1) move to positions
+ *   ctx_len[s] + i: the accepted path of a tree, or what stays of a cache that drops tokens (with
+ *   ctx_len 0).  Keys are not turned again: a path's tokens have the depths 0, 1, 2, ...  The list
+ *   ends before an entry that does not rise or is out of range; n_keep is taken within 0 .. new tokens.
+ *   The positions behind the moved tokens hold nothing that is meant to be read.  A scale block
+ *   that receives tokens gets the largest of the scales that they and its tokens before ctx_len
+ *   come with (a NaN if there is one), and codes that come with another become
+ *   round-half-even(code * (their scale / new scale)); with scale_block 1 nothing is rounded.  A
+ *   kept token on a page that does not exist moves as zeros, one to such a page is dropped.  From the
+ *   scale block that holds ctx_len on, pages belong to one sequence of the batch.
+ * Every cache array 16-byte aligned, the others 4-byte.
+ */
+catq_status catq_aux_kv_copy_pages(const catq_kv_desc* d, const catq_kv_cache* cache, const int32_t* src,
+                                   const int32_t* dst, int64_t n, hipStream_t stream);
+catq_status catq_aux_kv_compact(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                const catq_kv_batch* batch, const int32_t* keep, const int32_t* n_keep,
+                                hipStream_t stream);
+
 /* SwiGLU on gu [rows][2F] (gate | up): a = silu(gate) * up, [rows][F]. */
 catq_status catq_aux_swiglu_fwd(const void* gu, int64_t rows, int64_t F, void* a,
                                 hipStream_t stream);

@@ -12,7 +12,7 @@ import torch
 
 from . import _lib
 from ._lib import (BF16, F32, HARD, IDENTITY, SOFT, WS_LINEAR_BWD, WS_LOSS, AttnDesc, CatqError,
-                   KvBatch, KvCache, KvDesc, KvPrep, LmstParams)
+                   KvBatch, KvCache, KvDesc, KvPrep, KvTree, LmstParams)
 
 __all__ = [
     "catq_modulate_ternarize", "catq_fakeq_linear_fwd", "catq_fakeq_linear_bwd",
@@ -26,7 +26,8 @@ __all__ = [
     "catq_aux_moe_combine_bwd", "catq_aux_moe_scatter_add", "catq_aux_adamw", "catq_aux_add",
     "catq_ternary_linear_a8", "catq_aux_rmsnorm_quant", "catq_aux_act_quant8", "catq_aux_kv_append",
     "catq_aux_kv_read", "catq_aux_paged_attention", "catq_paged_attention_workspace_bytes",
-    "kv_desc", "kv_cache", "kv_batch", "kv_prep", "KvDesc", "KvCache", "KvBatch", "KvPrep",
+    "catq_aux_kv_append_tree", "catq_aux_tree_attention", "catq_aux_kv_copy_pages", "catq_aux_kv_compact",
+    "kv_desc", "kv_cache", "kv_batch", "kv_prep", "kv_tree", "KvDesc", "KvCache", "KvBatch", "KvPrep", "KvTree",
     "lmst_params", "attn_desc", "IDENTITY", "SOFT", "HARD", "F32", "BF16", "CatqError",
     "LmstParams", "AttnDesc", "lib", "catq_trace_enable", "catq_trace_pause",
     "catq_trace_reset", "catq_trace_count", "catq_trace_get", "catq_trace_disable",
@@ -503,9 +504,32 @@ def _kv_same(desc, cache, batch):
     return dev
 
 
-def catq_aux_kv_append(desc, cache, batch, prep, qkv, q_out, stream=None):
-    """New tokens' qkv [n_tokens][(n_q + 2 n_kv) head_dim] (bf16): normed and rotated
-    q into q_out [n_tokens][n_q head_dim], k and v into the cache."""
+def kv_tree(batch, mask=None, depth=None):
+    """The new tokens of a batch as trees (see catq_kv_tree in the header): mask int64
+    [n_tokens][words] (64 bits a word; needed for the attention), depth int32 [n_tokens] or
+    None.  The returned struct keeps the tensors."""
+    n, dev, words = batch.n_tokens, batch.device, -(-batch.max_new // 64) or 1
+    if mask is not None:
+        if mask.dim() != 2:
+            raise ValueError(f"mask: {mask.dim()} dimensions, expected 2")
+        words = mask.shape[1]
+        _int32(words=words)
+        _want(mask, "mask", torch.int64, (n, words), dev)
+    if depth is not None:
+        _want(depth, "depth", torch.int32, (n,), dev)
+    t = KvTree(_ptr(mask), _ptr(depth), words)
+    t.tensors, t.device, t.rows = (mask, depth), dev, n
+    return t
+
+
+def _tree_same(tree, batch):
+    if tree.device != batch.device:
+        raise ValueError(f"tree: on GPU {tree.device}, expected {batch.device}")
+    if tree.rows != batch.n_tokens:
+        raise ValueError(f"tree: made for {tree.rows} tokens, expected {batch.n_tokens}")
+
+
+def _append_checks(desc, cache, batch, prep, qkv, q_out):
     dev, n, d = _kv_same(desc, cache, batch), batch.n_tokens, desc.head_dim
     if prep.device is not None and prep.device != dev:
         raise ValueError(f"prep: on GPU {prep.device}, expected {dev}")
@@ -513,8 +537,44 @@ def catq_aux_kv_append(desc, cache, batch, prep, qkv, q_out, stream=None):
         raise ValueError(f"prep: made for heads of {prep.width} values, expected {d}")
     _want(qkv, "qkv", torch.bfloat16, (n, (desc.n_q + 2 * desc.n_kv) * d), dev)
     _want(q_out, "q_out", torch.bfloat16, (n, desc.n_q * d), dev)
+    return dev
+
+
+def catq_aux_kv_append(desc, cache, batch, prep, qkv, q_out, stream=None):
+    """New tokens' qkv [n_tokens][(n_q + 2 n_kv) head_dim] (bf16): normed and rotated
+    q into q_out [n_tokens][n_q head_dim], k and v into the cache."""
+    dev = _append_checks(desc, cache, batch, prep, qkv, q_out)
     _run_on(dev, stream, lib.catq_aux_kv_append, "catq_aux_kv_append", C.byref(desc), C.byref(cache),
             C.byref(batch), C.byref(prep), _ptr(qkv), _ptr(q_out))
+
+
+def catq_aux_kv_append_tree(desc, cache, batch, tree, prep, qkv, q_out, stream=None):
+    """catq_aux_kv_append for a tree of drafted tokens, each rotated for its depth."""
+    dev = _append_checks(desc, cache, batch, prep, qkv, q_out)
+    _tree_same(tree, batch)
+    _run_on(dev, stream, lib.catq_aux_kv_append_tree, "catq_aux_kv_append_tree", C.byref(desc), C.byref(cache),
+            C.byref(batch), C.byref(tree), C.byref(prep), _ptr(qkv), _ptr(q_out))
+
+
+def catq_aux_kv_copy_pages(desc, cache, src, dst, stream=None):
+    """Pages dst (int32 [n], on the device) become copies of pages src."""
+    dev, n = cache.device, src.numel()
+    if bytes(desc)[:24] != cache.geometry:
+        raise ValueError("the cache was made for another descriptor")
+    _want(src, "src", torch.int32, (n,), dev)
+    _want(dst, "dst", torch.int32, (n,), dev)
+    _run_on(dev, stream, lib.catq_aux_kv_copy_pages, "catq_aux_kv_copy_pages", C.byref(desc), C.byref(cache),
+            _ptr(src), _ptr(dst), n)
+
+
+def catq_aux_kv_compact(desc, cache, batch, keep, n_keep, stream=None):
+    """The new tokens named by keep (int32 [n_tokens], n_keep [n_seqs] of them per sequence, rising) move to
+    the front of their sequence's new ones."""
+    dev = _kv_same(desc, cache, batch)
+    _want(keep, "keep", torch.int32, (batch.n_tokens,), dev)
+    _want(n_keep, "n_keep", torch.int32, (batch.n_seqs,), dev)
+    _run_on(dev, stream, lib.catq_aux_kv_compact, "catq_aux_kv_compact", C.byref(desc), C.byref(cache),
+            C.byref(batch), _ptr(keep), _ptr(n_keep))
 
 
 def catq_aux_kv_read(desc, cache, batch, k_out=None, v_out=None, stream=None):
@@ -531,9 +591,7 @@ def catq_paged_attention_workspace_bytes(desc, batch):
     return int(lib.catq_paged_attention_workspace_bytes(C.byref(desc), C.byref(batch)))
 
 
-def catq_aux_paged_attention(desc, cache, batch, q, o, workspace=None, scale=None, lse=None, stream=None):
-    """Attention of the new tokens' q over the cache that holds them (scale None:
-    1/sqrt(head_dim)); o like q, lse fp32 [n_tokens][n_q] or None."""
+def _attention_checks(desc, cache, batch, q, o, workspace, lse):
     dev, shape = _kv_same(desc, cache, batch), (batch.n_tokens, desc.n_q * desc.head_dim)
     _want(q, "q", torch.bfloat16, shape, dev)
     _want(o, "o", torch.bfloat16, shape, dev)
@@ -541,8 +599,25 @@ def catq_aux_paged_attention(desc, cache, batch, q, o, workspace=None, scale=Non
         _want(lse, "lse", torch.float32, (batch.n_tokens, desc.n_q), dev)
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError(f"workspace: must be contiguous and on GPU {dev}")
+    return dev
+
+
+def catq_aux_paged_attention(desc, cache, batch, q, o, workspace=None, scale=None, lse=None, stream=None):
+    """Attention of the new tokens' q over the cache that holds them (scale None:
+    1/sqrt(head_dim)); o like q, lse fp32 [n_tokens][n_q] or None."""
+    dev = _attention_checks(desc, cache, batch, q, o, workspace, lse)
     _run_on(dev, stream, lib.catq_aux_paged_attention, "catq_aux_paged_attention", C.byref(desc),
             C.byref(cache), C.byref(batch), _ptr(q), desc.head_dim ** -0.5 if scale is None else scale, _ptr(o),
+            _ptr(lse), _ptr(workspace), _bytes(workspace))
+
+
+def catq_aux_tree_attention(desc, cache, batch, tree, q, o, workspace=None, scale=None, lse=None, stream=None):
+    """catq_aux_paged_attention of a tree of drafted tokens: a row sees what was cached before and the new
+    tokens that its mask names."""
+    dev = _attention_checks(desc, cache, batch, q, o, workspace, lse)
+    _tree_same(tree, batch)
+    _run_on(dev, stream, lib.catq_aux_tree_attention, "catq_aux_tree_attention", C.byref(desc), C.byref(cache),
+            C.byref(batch), C.byref(tree), _ptr(q), desc.head_dim ** -0.5 if scale is None else scale, _ptr(o),
             _ptr(lse), _ptr(workspace), _bytes(workspace))
 
 

@@ -51,6 +51,10 @@ class KvPrep(C.Structure):
                 ("act_quant", C.c_int32), ("rope_scale", C.c_float), ("eps", C.c_float)]
 
 
+class KvTree(C.Structure):
+    _fields_ = [("mask", C.c_void_p), ("depth", C.c_void_p), ("words", C.c_int32)]
+
+
 class TraceRec(C.Structure):
     _fields_ = [("tag", C.c_char * 96), ("flops", C.c_double), ("bytes", C.c_double),
                 ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("ms", C.c_float)]
@@ -65,7 +69,7 @@ class CatqError(RuntimeError):
 P, I64, I32, F, SZ = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_size_t
 PP = C.POINTER(LmstParams)
 PA = C.POINTER(AttnDesc)
-PKD, PKC, PKB, PKP = (C.POINTER(s) for s in (KvDesc, KvCache, KvBatch, KvPrep))
+PKD, PKC, PKB, PKP, PKT = (C.POINTER(s) for s in (KvDesc, KvCache, KvBatch, KvPrep, KvTree))
 
 SIGNATURES = {
     "catq_modulate_ternarize": [P, I32, I64, I64, P, P, P, PP, P, I32, P, I32, P, P, P],
@@ -90,6 +94,10 @@ SIGNATURES = {
     "catq_aux_kv_read": [PKD, PKC, PKB, P, P, P],
     "catq_paged_attention_workspace_bytes": [PKD, PKB],
     "catq_aux_paged_attention": [PKD, PKC, PKB, P, F, P, P, P, SZ, P],
+    "catq_aux_kv_append_tree": [PKD, PKC, PKB, PKT, PKP, P, P, P],
+    "catq_aux_tree_attention": [PKD, PKC, PKB, PKT, P, F, P, P, P, SZ, P],
+    "catq_aux_kv_copy_pages": [PKD, PKC, P, P, I64, P],
+    "catq_aux_kv_compact": [PKD, PKC, PKB, P, P, P],
     "catq_aux_rmsnorm_fwd": [P, I32, I64, I64, F, P, P, P],
     "catq_aux_rmsnorm_bwd": [P, I32, P, P, P, I64, I64, P, P],
     "catq_attn_saved_bytes": [PA],

@@ -23,8 +23,16 @@
 
 namespace catq {
 
-catq_status kv_check_sizes(const catq_kv_desc* d, const catq_kv_batch* b) {
-  CATQ_REQUIRE(d && b, CATQ_ERR_NULL, "descriptor and batch must not be NULL");
+catq_status kv_check_pool(const catq_kv_desc* d, const catq_kv_cache* c) {
+  CATQ_TRY(kv_check_desc(d));
+  CATQ_REQUIRE(c && c->k && c->v && c->k_scale && c->v_scale, CATQ_ERR_NULL, "cache arrays must not be NULL");
+  CATQ_REQUIRE(aligned16(c->k) && aligned16(c->v) && aligned16(c->k_scale) && aligned16(c->v_scale),
+               CATQ_ERR_ALIGN, "cache arrays must be 16-byte aligned");
+  return CATQ_OK;
+}
+
+catq_status kv_check_desc(const catq_kv_desc* d) {
+  CATQ_REQUIRE(d, CATQ_ERR_NULL, "descriptor must not be NULL");
   CATQ_REQUIRE(d->n_q > 0 && d->n_kv > 0 && d->n_q % d->n_kv == 0 && d->n_q <= 1024,
                CATQ_ERR_SHAPE, "n_q must be a multiple of n_kv and at most 1024");
   CATQ_REQUIRE(d->head_dim == 64 || d->head_dim == 128 || d->head_dim == 256, CATQ_ERR_SHAPE,
@@ -37,11 +45,17 @@ catq_status kv_check_sizes(const catq_kv_desc* d, const catq_kv_batch* b) {
   CATQ_REQUIRE(d->n_pages > 0 && d->max_pages > 0 &&
                    count_ok((int64_t)d->n_pages * ps, d->n_kv, d->head_dim),
                CATQ_ERR_SHAPE, "n_pages and max_pages must be > 0, the pool within 2^38 elements");
+  return CATQ_OK;
+}
+
+catq_status kv_check_sizes(const catq_kv_desc* d, const catq_kv_batch* b) {
+  CATQ_REQUIRE(d && b, CATQ_ERR_NULL, "descriptor and batch must not be NULL");
+  CATQ_TRY(kv_check_desc(d));
   CATQ_REQUIRE(b->n_seqs >= 0 && b->n_tokens >= 0 && b->max_new >= 0 && b->max_len >= 0,
                CATQ_ERR_SHAPE, "batch sizes must be >= 0");
   CATQ_REQUIRE(b->n_tokens <= INT32_MAX && b->n_seqs <= 65535 && b->max_new <= (1 << 24),
                CATQ_ERR_SHAPE, "at most 2^31 - 1 tokens, 65535 sequences and 2^24 new tokens in one");
-  CATQ_REQUIRE(b->max_len <= (int64_t)d->max_pages * ps, CATQ_ERR_SHAPE,
+  CATQ_REQUIRE(b->max_len <= (int64_t)d->max_pages * d->page_size, CATQ_ERR_SHAPE,
                "max_len exceeds what max_pages pages hold");
   CATQ_REQUIRE(b->n_tokens == 0 ||
                    count_ok(b->n_tokens, d->n_q + 2 * (int64_t)d->n_kv, d->head_dim),
@@ -51,14 +65,21 @@ catq_status kv_check_sizes(const catq_kv_desc* d, const catq_kv_batch* b) {
 
 catq_status kv_check(const catq_kv_desc* d, const catq_kv_cache* c, const catq_kv_batch* b) {
   CATQ_TRY(kv_check_sizes(d, b));
-  CATQ_REQUIRE(c && c->k && c->v && c->k_scale && c->v_scale, CATQ_ERR_NULL, "cache arrays must not be NULL");
+  CATQ_TRY(kv_check_pool(d, c));
   CATQ_REQUIRE(b->n_seqs == 0 || (b->page_table && b->cu_new && b->ctx_len), CATQ_ERR_NULL,
                "batch arrays must not be NULL");
-  CATQ_REQUIRE(aligned16(c->k) && aligned16(c->v) && aligned16(c->k_scale) && aligned16(c->v_scale),
-               CATQ_ERR_ALIGN, "cache arrays must be 16-byte aligned");
   CATQ_REQUIRE(((reinterpret_cast<uintptr_t>(b->page_table) | reinterpret_cast<uintptr_t>(b->cu_new) |
                  reinterpret_cast<uintptr_t>(b->ctx_len)) & 3) == 0,
                CATQ_ERR_ALIGN, "batch arrays must be 4-byte aligned");
+  return CATQ_OK;
+}
+
+catq_status kv_check_tree(const catq_kv_batch* b, const catq_kv_tree* t) {
+  CATQ_REQUIRE(t, CATQ_ERR_NULL, "tree must not be NULL");
+  CATQ_REQUIRE(t->words > 0 && t->words <= 1024 && (int64_t)t->words * 64 >= b->max_new, CATQ_ERR_SHAPE,
+               "a mask row needs 64-bit words for max_new tokens, and has at most 1024");
+  CATQ_REQUIRE((reinterpret_cast<uintptr_t>(t->mask) & 7) == 0 && (reinterpret_cast<uintptr_t>(t->depth) & 3) == 0,
+               CATQ_ERR_ALIGN, "mask must be 8-byte aligned, depth 4-byte");
   return CATQ_OK;
 }
 
@@ -76,6 +97,7 @@ struct AppendArgs {
   const float* inv_freq;
   const bf16* q_w;
   const bf16* k_w;
+  const int32_t* depth;   // TREE: a token's position is that much past its sequence's cached tokens
   const bf16* qkv;
   bf16* q_out;
   int32_t rot, inter, qk_norm, act_quant;
@@ -104,15 +126,20 @@ __device__ __forceinline__ uint64_t turn_fraction(float f) {
 // else is below 2^-31.  (Two floats with the whole turns taken off in an fma take the same time, 56 us
 // for the prompts above with their read back, and were off by 2^-24, more at frequencies above 1.)
 // Frequencies of 2^20 and above, infinite and NaN ones give NaN.
-__device__ __forceinline__ void angles(const AppendArgs& a, int64_t pos0, int n, float2* cs) {
+// TREE: the positions are ctx + depth[t] instead (a product per token in the place of a sum: 64 bits modulo
+// 2^64 as before).
+template <bool TREE>
+__device__ __forceinline__ void angles(const AppendArgs& a, int64_t pos0, int n, float2* cs,
+                                       const int32_t* depth = nullptr) {
   const int half = a.rot >> 1;
   for (int f = threadIdx.x & 63; f < half; f += 64) {
     const float freq = a.inv_freq[f];
     const bool fine = fabsf(freq) < 0x1p20f;
     const float scale = fine ? a.rope_scale : __builtin_nanf("");
     const uint64_t turn = turn_fraction(fine ? freq : 0.f);
-    uint64_t at = turn * (uint64_t)pos0;
+    uint64_t at = TREE ? 0 : turn * (uint64_t)pos0;
     for (int t = 0; t < n; ++t, at += turn) {
+      if constexpr (TREE) at = turn * (uint64_t)(pos0 + depth[t]);
       float s, c;
       sincospif((float)(int32_t)(at >> 32) * 0x1p-31f, &s, &c);   // (of twice the fraction, in [-1, 1])
       cs[t * half + f] = make_float2(c * scale, s * scale);
@@ -190,7 +217,7 @@ __device__ __forceinline__ void prep_head(const AppendArgs& a, float (&v)[16], i
 
 // One token and as many heads as fit the workgroup. (Four tokens a workgroup were slower, 62 us
 // against 55 for the prompts above.)
-template <int LPH>
+template <int LPH, bool TREE>
 __device__ __forceinline__ void append_q(const AppendArgs& a, int64_t block, float2* cs, int64_t* s_pos) {
   constexpr int D = LPH * 16, HP = 256 / LPH;   // heads per workgroup
   const int64_t t = block / a.q_parts;
@@ -214,12 +241,12 @@ __device__ __forceinline__ void append_q(const AppendArgs& a, int64_t block, flo
     }
     const KvSeq q = kv_seq(a.g, lo);
     // (a row of no sequence)
-    *s_pos = t < q.row0 || t >= q.row0 + q.n ? INT64_MIN : q.ctx + (t - q.row0);
+    *s_pos = t < q.row0 || t >= q.row0 + q.n ? INT64_MIN : q.ctx + (TREE ? a.depth[t] : t - q.row0);
   }
   __syncthreads();
   const int64_t pos = *s_pos;
   if (pos == INT64_MIN) return;
-  if (threadIdx.x < 64) angles(a, pos, 1, cs);
+  if (threadIdx.x < 64) angles<false>(a, pos, 1, cs);
   __syncthreads();
   prep_head<LPH>(a, v, sub, hp, a.q_w, cs);
   if (a.act_quant) {
@@ -250,7 +277,7 @@ __device__ __forceinline__ float code_of(unsigned int w, int b) {
 }
 
 // LPH lanes per head, NP passes of TP = 256 / LPH tokens (or one of fewer)
-template <int LPH, int NP>
+template <int LPH, int NP, bool TREE>
 __device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, float2* cs,
                                           unsigned int* s_mag, float* s_scale, float* s_ratio,
                                           unsigned char* s_tile) {
@@ -301,7 +328,13 @@ __device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, fl
       // of the pass's new tokens, a quarter by each wave
       const int ta = max(lo - p * TP, 0), n = min(hi - p * TP, TP) - ta, w = threadIdx.x >> 6;
       const int w0 = n * w >> 2, w1 = n * (w + 1) >> 2;
-      if (n > 0) angles(a, first + p * TP + ta + w0, w1 - w0, cs + (ta + w0) * (a.rot >> 1));
+      if (n > 0) {
+        const int64_t at = first + p * TP + ta + w0;
+        if constexpr (TREE)
+          angles<true>(a, q.ctx, w1 - w0, cs + (ta + w0) * (a.rot >> 1), a.depth + q.row0 + (at - q.ctx));
+        else
+          angles<false>(a, at, w1 - w0, cs + (ta + w0) * (a.rot >> 1));
+      }
       __syncthreads();
       prep_head<LPH>(a, v[p], sub, hp, a.k_w, cs + tl * (a.rot >> 1));
       if (t < lo || t >= hi)        // (a norm turns zeros into zeros, an angle may be anything)
@@ -389,7 +422,7 @@ __device__ __forceinline__ void append_kv(const AppendArgs& a, int64_t block, fl
   }
 }
 
-template <int LPH, int NP>
+template <int LPH, int NP, bool TREE>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   constexpr int D = LPH * 16, TP = 256 / LPH;
   __shared__ float2 cs[TP * D / 2];
@@ -400,9 +433,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   __shared__ __align__(16) unsigned char s_tile[TP * NP * D];
   const int64_t b = blockIdx.x;
   if (b < a.kv_blocks)
-    append_kv<LPH, NP>(a, b, cs, s_mag, s_scale, s_ratio, s_tile);
+    append_kv<LPH, NP, TREE>(a, b, cs, s_mag, s_scale, s_ratio, s_tile);
   else
-    append_q<LPH>(a, b - a.kv_blocks, cs, &s_pos);
+    append_q<LPH, TREE>(a, b - a.kv_blocks, cs, &s_pos);
 }
 
 // Eight values of one (token, head) per thread.  A v word holds four tokens: the
@@ -458,9 +491,10 @@ catq_status launch_append(const AppendArgs& a, int64_t blocks, double bytes, hip
   constexpr int TP = 256 / LPH;
   auto go = [&](auto np) {
     constexpr int NP = decltype(np)::value;
-    CATQ_TRACED(stream, "kv_append_kernel", 0.0, bytes, a.g.n_tokens, a.g.n_q + 2 * a.g.n_kv, a.g.d,
-                hipLaunchKernelGGL((kv_append_kernel<LPH, NP>), dim3((unsigned)blocks), dim3(256), 0,
-                                   stream, a));
+    auto kernel = a.depth ? kv_append_kernel<LPH, NP, true> : kv_append_kernel<LPH, NP, false>;
+    CATQ_TRACED(stream, a.depth ? "kv_append_kernel<tree>" : "kv_append_kernel", 0.0, bytes, a.g.n_tokens,
+                a.g.n_q + 2 * a.g.n_kv, a.g.d,
+                hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a));
   };
   using std::integral_constant;
   const int passes = ((1 << a.w_log2) + TP - 1) / TP;   // a power of two
@@ -481,16 +515,9 @@ catq_status launch_append(const AppendArgs& a, int64_t blocks, double bytes, hip
   return CATQ_OK;
 }
 
-}  // namespace
-}  // namespace catq
-
-using namespace catq;
-
-extern "C" catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_cache* cache,
-                                          const catq_kv_batch* batch, const catq_kv_prep* prep,
-                                          const void* qkv, void* q_out, hipStream_t stream) {
-  clear_error();
-  CATQ_TRY(kv_check(d, cache, batch));
+catq_status append(const catq_kv_desc* d, const catq_kv_cache* cache, const catq_kv_batch* batch,
+                   const int32_t* depth, const catq_kv_prep* prep, const void* qkv, void* q_out,
+                   hipStream_t stream) {
   CATQ_REQUIRE(prep, CATQ_ERR_NULL, "prep must not be NULL");
   CATQ_REQUIRE(prep->rot_dim >= 0 && prep->rot_dim <= d->head_dim && prep->rot_dim % 16 == 0,
                CATQ_ERR_SHAPE, "rot_dim must be a multiple of 16, at most head_dim");
@@ -509,6 +536,7 @@ extern "C" catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_c
   a.inv_freq = prep->inv_freq;
   a.q_w = static_cast<const bf16*>(prep->q_weight);
   a.k_w = static_cast<const bf16*>(prep->k_weight);
+  a.depth = depth;
   a.qkv = static_cast<const bf16*>(qkv);
   a.q_out = static_cast<bf16*>(q_out);
   a.rot = prep->rot_dim;
@@ -536,6 +564,29 @@ extern "C" catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_c
     case 8: return launch_append<8>(a, blocks, bytes, stream);
     default: return launch_append<16>(a, blocks, bytes, stream);
   }
+}
+
+}  // namespace
+}  // namespace catq
+
+using namespace catq;
+
+extern "C" catq_status catq_aux_kv_append(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                          const catq_kv_batch* batch, const catq_kv_prep* prep,
+                                          const void* qkv, void* q_out, hipStream_t stream) {
+  clear_error();
+  CATQ_TRY(kv_check(d, cache, batch));
+  return append(d, cache, batch, nullptr, prep, qkv, q_out, stream);
+}
+
+extern "C" catq_status catq_aux_kv_append_tree(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                               const catq_kv_batch* batch, const catq_kv_tree* tree,
+                                               const catq_kv_prep* prep, const void* qkv, void* q_out,
+                                               hipStream_t stream) {
+  clear_error();
+  CATQ_TRY(kv_check(d, cache, batch));
+  CATQ_TRY(kv_check_tree(batch, tree));
+  return append(d, cache, batch, tree->depth, prep, qkv, q_out, stream);
 }
 
 extern "C" catq_status catq_aux_kv_read(const catq_kv_desc* d, const catq_kv_cache* cache,

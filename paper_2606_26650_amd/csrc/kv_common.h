@@ -47,6 +47,9 @@ __device__ __forceinline__ int64_t kv_scale_index(const KvGeom& g, int page, int
   return (((int64_t)page * g.n_kv + h) << (g.ps_log2 - g.bt_log2)) + (tok >> g.bt_log2);
 }
 
+catq_status kv_check_desc(const catq_kv_desc* d);
+catq_status kv_check_pool(const catq_kv_desc* d, const catq_kv_cache* c);
+catq_status kv_check_tree(const catq_kv_batch* b, const catq_kv_tree* t);
 catq_status kv_check(const catq_kv_desc* d, const catq_kv_cache* c, const catq_kv_batch* b);
 catq_status kv_check_sizes(const catq_kv_desc* d, const catq_kv_batch* b);
 KvGeom kv_geom(const catq_kv_desc* d, const catq_kv_batch* b);

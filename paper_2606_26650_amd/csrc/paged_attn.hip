@@ -65,6 +65,8 @@ struct PaArgs {
   int32_t spans;
   int32_t span;      // tokens of a span: a multiple of 128
   int32_t limit;     // no position from here on is read: the pages' and the spans' end
+  const uint64_t* mask;   // TREE: [token][words], the new tokens of its sequence that a row sees
+  int32_t words;
   float c;           // softmax scale * log2(e)
 };
 
@@ -108,13 +110,29 @@ __device__ __forceinline__ float col_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
-// tokens that new token i of sequence q sees
+// Tokens that new token i of sequence q sees: the positions below this. TREE: of those, the ones before the
+// new tokens (visible_all) and the new ones whose bit its mask has.
+template <bool TREE>
 __device__ __forceinline__ int visible(const PaArgs& a, const KvSeq& q, int i) {
-  const int64_t v = min((int64_t)q.ctx + i + 1, (int64_t)a.limit);
+  const int64_t v = min((int64_t)q.ctx + (TREE ? q.n : i + 1), (int64_t)a.limit);
   return v < 0 ? 0 : (int)v;
 }
+template <bool TREE>
+__device__ __forceinline__ int visible_all(const PaArgs& a, const KvSeq& q, int i) {
+  return TREE ? max(min(q.ctx, a.limit), 0) : visible<false>(a, q, i);
+}
+// Whether a row sees new tokens j .. j + 3, as four bits; the ones before the new tokens (j < 0) are seen, the
+// ones behind the mask are not.
+__device__ __forceinline__ unsigned int seen4(const uint64_t* row, int words, int j) {
+  if (j < 0) return j <= -4 ? 15u : (((unsigned)row[0] << -j) | ((1u << -j) - 1u)) & 15u;
+  const int w = j >> 6, s = j & 63;
+  if (w >= words) return 0u;
+  unsigned int b = (unsigned)(row[w] >> s);
+  if (s > 60 && w + 1 < words) b |= (unsigned)(row[w + 1] << (64 - s));
+  return b & 15u;
+}
 
-template <int D, int NR, bool PER_TOKEN>
+template <int D, int NR, bool PER_TOKEN, bool TREE>
 __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
   constexpr int HH = D / 64;          // 64-value halves of a head
   constexpr int NT = D / 16;          // output tiles
@@ -134,11 +152,11 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
   const int rows = q.n * a.G, r0 = rt * 16 * NR;
   if (r0 >= rows) return;
   const int last = min(r0 + 16 * NR, rows) - 1;
-  const int vmax = visible(a, q, last / a.G);
+  const int vmax = visible<TREE>(a, q, last / a.G);
   const int c0 = sp * a.span;
   if (sp > 0 && c0 >= vmax) return;      // the join knows which spans are there
   const int c1 = min(vmax, c0 + a.span);
-  const int vmin = visible(a, q, r0 / a.G);   // every row of the tile sees that much
+  const int vmin = visible_all<TREE>(a, q, r0 / a.G);   // every row of the tile sees that much
 
   // queries: fp16 of q over the power of two at its row's largest magnitude. A row with a NaN or an
   // infinity in it (or a magnitude that passes fp32 times the softmax scale) is taken as zeros and made
@@ -146,12 +164,14 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
   f16x8 qf[NR][2 * HH];
   float qc[NR];        // that power times the softmax scale, in log2 units
   int vis[NR];
+  const uint64_t* mrow[TREE ? NR : 1];
   bool odd[NR];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     const int row = min(r0 + 16 * r + lm, rows - 1);
     const int i = row / a.G, hq = h * a.G + (row - i * a.G);
-    vis[r] = visible(a, q, i);
+    vis[r] = visible<TREE>(a, q, i);
+    if constexpr (TREE) mrow[r] = a.mask + (q.row0 + i) * a.words;
     const bf16* qp = a.Q + ((q.row0 + i) * g.n_q + hq) * D + 16 * lg;
     float v[HH][16];
     float m = 0.f;
@@ -297,9 +317,11 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
           x[u][i] = fmaf(acc[i], ksc[u][si] * qc[r], lv[u][si]);
         }
         if (edge) {
+          unsigned int seen = 15u;
+          if constexpr (TREE) seen = seen4(mrow[r], a.words, tok + 16 * u + 4 * lg - q.ctx);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (masked[u] || tok + 16 * u + 4 * lg + i >= vis[r]) x[u][i] = -INFINITY;
+            if (masked[u] || tok + 16 * u + 4 * lg + i >= vis[r] || !((seen >> i) & 1u)) x[u][i] = -INFINITY;
         }
       }
       float mx = x[0][0];
@@ -424,7 +446,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
 constexpr int kTile = 64, kPitch = kTile + 1;
 constexpr float kTinyLog = -61.0f;
 
-template <int D, int NW, bool PER_TOKEN>
+template <int D, int NW, bool PER_TOKEN, bool TREE>
 __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
   constexpr int KS = D / 16;            // contraction slices of the scores
   constexpr int DB = D / 32;            // output blocks
@@ -445,7 +467,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
   const KvSeq q = kv_seq(g, s);
   const int rows = q.n * a.G, r0 = rt * kRows;
   if (r0 >= rows) return;
-  const int vmax = visible(a, q, (min(r0 + kRows, rows) - 1) / a.G);
+  const int vmax = visible<TREE>(a, q, (min(r0 + kRows, rows) - 1) / a.G);
   const int c0 = sp * a.span;
   if (sp > 0 && c0 >= vmax) return;      // the join knows which spans are there
   const int c1 = min(vmax, c0 + a.span);
@@ -453,9 +475,10 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
   const int w0 = r0 + 32 * wave;
   const bool has_rows = w0 < rows;
   const int row = min(w0 + l32, rows - 1), qi = row / a.G, hq = h * a.G + (row - qi * a.G);
-  const int vis = visible(a, q, qi);
-  const int wmin = visible(a, q, min(w0, rows - 1) / a.G);
-  const int wmax = has_rows ? visible(a, q, min(w0 + 31, rows - 1) / a.G) : 0;
+  const int vis = visible<TREE>(a, q, qi);
+  const int wmin = visible_all<TREE>(a, q, min(w0, rows - 1) / a.G);
+  const int wmax = has_rows ? visible<TREE>(a, q, min(w0 + 31, rows - 1) / a.G) : 0;
+  const uint64_t* mrow = TREE ? a.mask + (q.row0 + qi) * a.words : nullptr;
 
   // queries as above; the score of a token on a missing page is then -inf whatever the query is.
   // (Setting those scores in the loop took 396 us for the prompt chunks above where this takes 386.)
@@ -644,8 +667,14 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (t0 + 32 * u + 8 * (i >> 2) + 4 * hh + (i & 3) >= vis) x[u][i] = -INFINITY;
+        for (int qd = 0; qd < 4; ++qd) {
+          const int t = t0 + 32 * u + 8 * qd + 4 * hh;
+          unsigned int seen = 15u;
+          if constexpr (TREE) seen = seen4(mrow, a.words, t - q.ctx);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t + e >= vis || !((seen >> e) & 1u)) x[u][4 * qd + e] = -INFINITY;
+        }
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -741,7 +770,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
 // (With a running maximum over the spans instead, 256 spans took 12 us.)
 constexpr int kMaxSpans = 512;
 
-template <int D>
+template <int D, bool TREE>
 __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
   constexpr int LN = D / 4, GR = 256 / LN;
   __shared__ __align__(16) float s_o[GR][D];
@@ -759,7 +788,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
   if (t < q.row0 || t >= q.row0 + q.n) return;
   const int i = (int)(t - q.row0);
   const int r0 = (i * a.G + hq % a.G) / a.tile_rows * a.tile_rows;
-  const int vmax = visible(a, q, (min(r0 + a.tile_rows, q.n * a.G) - 1) / a.G);
+  const int vmax = visible<TREE>(a, q, (min(r0 + a.tile_rows, q.n * a.G) - 1) / a.G);
   const int live = max((vmax + a.span - 1) / a.span, 1);
   const int64_t at = t * g.n_q + hq, step = g.n_tokens * g.n_q;
   float M = kNone;
@@ -843,26 +872,26 @@ Plan plan(const catq_kv_desc* d, const catq_kv_batch* b) {
   return p;
 }
 
-template <int D>
+template <int D, bool TREE>
 catq_status launch_paged(const PaArgs& a, bool per_token, double flops, double bytes, hipStream_t stream) {
   const dim3 grid((unsigned)((int64_t)a.row_tiles * a.spans * a.g.n_kv), (unsigned)a.g.n_seqs);
   char tag[64];
-  trace_tag(tag, sizeof tag, "paged_attn<%d rows, head_dim %d>", a.tile_rows, D);
+  trace_tag(tag, sizeof tag, "paged_attn<%d rows, head_dim %d%s>", a.tile_rows, D, TREE ? ", tree" : "");
   auto go = [&](auto kernel) {
     CATQ_TRACED(stream, tag, flops, bytes, a.g.n_tokens, a.g.n_q, D,
                 hipLaunchKernelGGL(kernel, grid, dim3(a.tile_rows == 256 ? 512 : 256), 0, stream, a));
   };
-  if (a.tile_rows == 16) per_token ? go(paged_attn_kernel<D, 1, true>) : go(paged_attn_kernel<D, 1, false>);
-  else if (a.tile_rows == 32) per_token ? go(paged_attn_kernel<D, 2, true>) : go(paged_attn_kernel<D, 2, false>);
+  if (a.tile_rows == 16) per_token ? go(paged_attn_kernel<D, 1, true, TREE>) : go(paged_attn_kernel<D, 1, false, TREE>);
+  else if (a.tile_rows == 32) per_token ? go(paged_attn_kernel<D, 2, true, TREE>) : go(paged_attn_kernel<D, 2, false, TREE>);
   else if constexpr (D <= 128) {
-    if (a.tile_rows == 128) per_token ? go(paged_tile_kernel<D, 4, true>) : go(paged_tile_kernel<D, 4, false>);
-    else per_token ? go(paged_tile_kernel<D, 8, true>) : go(paged_tile_kernel<D, 8, false>);
+    if (a.tile_rows == 128) per_token ? go(paged_tile_kernel<D, 4, true, TREE>) : go(paged_tile_kernel<D, 4, false, TREE>);
+    else per_token ? go(paged_tile_kernel<D, 8, true, TREE>) : go(paged_tile_kernel<D, 8, false, TREE>);
   }
   CATQ_CHECK_LAUNCH("paged attention");
   if (a.spans > 1) {
     CATQ_TRACED(stream, "paged_join_kernel", 0.0, (double)a.g.n_tokens * a.g.n_q * D * (4.0 * a.spans + 2.0),
                 a.g.n_tokens, a.g.n_q, D,
-                hipLaunchKernelGGL((paged_join_kernel<D>), dim3((unsigned)(a.g.n_tokens * a.g.n_q)), dim3(256), 0,
+                hipLaunchKernelGGL((paged_join_kernel<D, TREE>), dim3((unsigned)(a.g.n_tokens * a.g.n_q)), dim3(256), 0,
                                    stream, a));
     CATQ_CHECK_LAUNCH("paged attention join");
   }
@@ -875,25 +904,13 @@ size_t plan_bytes(const catq_kv_desc* d, const catq_kv_batch* b, const Plan& p) 
   return round_up(rows * (size_t)d->head_dim * 4, 256) + round_up(rows * 8, 256);
 }
 
-}  // namespace
-}  // namespace catq
-
-using namespace catq;
-
-extern "C" size_t catq_paged_attention_workspace_bytes(const catq_kv_desc* d, const catq_kv_batch* b) {
-  if (kv_check_sizes(d, b) != CATQ_OK || b->n_seqs == 0 || b->n_tokens == 0 || b->max_new == 0) return 0;
-  return plan_bytes(d, b, plan(d, b));
-}
-
-extern "C" catq_status catq_aux_paged_attention(const catq_kv_desc* d, const catq_kv_cache* cache,
-                                                const catq_kv_batch* batch, const void* q, float scale,
-                                                void* o, float* lse, void* workspace,
-                                                size_t workspace_bytes, hipStream_t stream) {
-  clear_error();
-  CATQ_TRY(kv_check(d, cache, batch));
+catq_status attend(const catq_kv_desc* d, const catq_kv_cache* cache, const catq_kv_batch* batch,
+                   const catq_kv_tree* tree, const void* q, float scale, void* o, float* lse, void* workspace,
+                   size_t workspace_bytes, hipStream_t stream) {
   CATQ_REQUIRE(scale >= 0.f && scale < 3.0e38f, CATQ_ERR_VALUE, "scale must be finite and >= 0");
   if (batch->n_seqs == 0 || batch->n_tokens == 0 || batch->max_new == 0) return CATQ_OK;
   CATQ_REQUIRE(q && o, CATQ_ERR_NULL, "q and o must not be NULL");
+  CATQ_REQUIRE(!tree || tree->mask, CATQ_ERR_NULL, "mask must not be NULL");
   CATQ_REQUIRE(aligned16(q) && aligned16(o) && aligned16(workspace) &&
                    (reinterpret_cast<uintptr_t>(lse) & 3) == 0,
                CATQ_ERR_ALIGN, "misaligned");
@@ -928,13 +945,51 @@ extern "C" catq_status catq_aux_paged_attention(const catq_kv_desc* d, const cat
   a.spans = p.spans;
   a.span = p.span;
   a.limit = (int32_t)std::min<int64_t>((int64_t)d->max_pages * d->page_size, (int64_t)p.spans * p.span);
+  if (tree) {
+    a.mask = tree->mask;
+    a.words = tree->words;
+  }
   a.c = scale * 1.44269504088896341f;
   const bool per_token = d->scale_block == 1;
   const double flops = 4.0 * (double)batch->n_tokens * batch->max_len * d->n_q * d->head_dim;
   const double bytes = 2.0 * (double)batch->n_seqs * batch->max_len * d->n_kv * d->head_dim;
+  auto go = [&](auto d_c) {
+    constexpr int D = decltype(d_c)::value;
+    return tree ? launch_paged<D, true>(a, per_token, flops, bytes, stream)
+                : launch_paged<D, false>(a, per_token, flops, bytes, stream);
+  };
   switch (d->head_dim) {
-    case 64: return launch_paged<64>(a, per_token, flops, bytes, stream);
-    case 128: return launch_paged<128>(a, per_token, flops, bytes, stream);
-    default: return launch_paged<256>(a, per_token, flops, bytes, stream);
+    case 64: return go(std::integral_constant<int, 64>{});
+    case 128: return go(std::integral_constant<int, 128>{});
+    default: return go(std::integral_constant<int, 256>{});
   }
+}
+
+}  // namespace
+}  // namespace catq
+
+using namespace catq;
+
+extern "C" size_t catq_paged_attention_workspace_bytes(const catq_kv_desc* d, const catq_kv_batch* b) {
+  if (kv_check_sizes(d, b) != CATQ_OK || b->n_seqs == 0 || b->n_tokens == 0 || b->max_new == 0) return 0;
+  return plan_bytes(d, b, plan(d, b));
+}
+
+extern "C" catq_status catq_aux_paged_attention(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                                const catq_kv_batch* batch, const void* q, float scale,
+                                                void* o, float* lse, void* workspace,
+                                                size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  CATQ_TRY(kv_check(d, cache, batch));
+  return attend(d, cache, batch, nullptr, q, scale, o, lse, workspace, workspace_bytes, stream);
+}
+
+extern "C" catq_status catq_aux_tree_attention(const catq_kv_desc* d, const catq_kv_cache* cache,
+                                               const catq_kv_batch* batch, const catq_kv_tree* tree,
+                                               const void* q, float scale, void* o, float* lse,
+                                               void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  CATQ_TRY(kv_check(d, cache, batch));
+  CATQ_TRY(kv_check_tree(batch, tree));
+  return attend(d, cache, batch, tree, q, scale, o, lse, workspace, workspace_bytes, stream);
 }
