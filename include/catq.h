@@ -587,6 +587,29 @@ catq_status catq_aux_kv_compact(const catq_kv_desc* d, const catq_kv_cache* cach
                                 const catq_kv_batch* batch, const int32_t* keep, const int32_t* n_keep,
                                 hipStream_t stream);
 
+/*
+ * catq_aux_sample: a token for each row of logits [rows][ld] (fp32 or bf16; V of them, V <= 2^20, ld >= V).
+ * Tokens are ordered by logit, the largest first, equal ones by index, and weigh
+ * w = exp((logit - largest) / temperature).  Kept are, one filter after the other,
+ *   top_k   the first top_k tokens (<= 0: all)
+ *   top_p   of these, those before which less than top_p of their weight lies (>= 1: all; the first always)
+ *   min_p   of these, those with w >= min_p (<= 0: all; the first always)
+ * and the row's token is the lowest index up to which the kept tokens of lower or equal index hold more than
+ * u of the kept weight; prob (NULL: not written) is its share of that.
+ *   temperature, top_p, min_p, u  fp32 [rows];  top_k  int32 [rows];  token  int32 [rows]; prob  fp32 [rows]
+ * The first four but u may be NULL (1, all, all, all).  u is taken within [0, 1 - 2^-24], a NaN as 0.  A
+ * temperature that is not above 0 takes the first token, with prob 1.  A NaN in top_p or min_p leaves that filter out.
+ * A logit that is NaN or -inf is never taken; where a row has no other, token is -1 and prob 0.  +inf logits share the
+ * whole weight.  Weights are held to 2^-43 of the largest, in integers: the result is the same every time.  The
+ * workspace (at least catq_aux_sample_workspace_bytes(rows, V) bytes; 0: may be NULL) is for one call at a time.
+ * logits and workspace 16-byte aligned, the others 4-byte.
+ */
+size_t catq_aux_sample_workspace_bytes(int64_t rows, int64_t V);
+catq_status catq_aux_sample(const void* logits, catq_dtype dtype, int64_t rows, int64_t V, int64_t ld,
+                            const float* temperature, const int32_t* top_k, const float* top_p,
+                            const float* min_p, const float* u, int32_t* token, float* prob,
+                            void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* SwiGLU on gu [rows][2F] (gate | up): a = silu(gate) * up, [rows][F]. */
 catq_status catq_aux_swiglu_fwd(const void* gu, int64_t rows, int64_t F, void* a,
                                 hipStream_t stream);

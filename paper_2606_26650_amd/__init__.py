@@ -27,6 +27,7 @@ __all__ = [
     "catq_ternary_linear_a8", "catq_aux_rmsnorm_quant", "catq_aux_act_quant8", "catq_aux_kv_append",
     "catq_aux_kv_read", "catq_aux_paged_attention", "catq_paged_attention_workspace_bytes",
     "catq_aux_kv_append_tree", "catq_aux_tree_attention", "catq_aux_kv_copy_pages", "catq_aux_kv_compact",
+    "catq_aux_sample", "catq_aux_sample_workspace_bytes",
     "kv_desc", "kv_cache", "kv_batch", "kv_prep", "kv_tree", "KvDesc", "KvCache", "KvBatch", "KvPrep", "KvTree",
     "lmst_params", "attn_desc", "IDENTITY", "SOFT", "HARD", "F32", "BF16", "CatqError",
     "LmstParams", "AttnDesc", "lib", "catq_trace_enable", "catq_trace_pause",
@@ -619,6 +620,31 @@ def catq_aux_tree_attention(desc, cache, batch, tree, q, o, workspace=None, scal
     _run_on(dev, stream, lib.catq_aux_tree_attention, "catq_aux_tree_attention", C.byref(desc), C.byref(cache),
             C.byref(batch), C.byref(tree), _ptr(q), desc.head_dim ** -0.5 if scale is None else scale, _ptr(o),
             _ptr(lse), _ptr(workspace), _bytes(workspace))
+
+
+def catq_aux_sample_workspace_bytes(rows, vocab):
+    return int(lib.catq_aux_sample_workspace_bytes(rows, vocab))
+
+
+def catq_aux_sample(logits, u, token, workspace=None, temperature=None, top_k=None, top_p=None, min_p=None,
+                    prob=None, stream=None):
+    """A token per row of logits [rows][V] (fp32 or bf16; rows may be strided) from the numbers u fp32 [rows]:
+    token int32 [rows], its probability prob fp32 [rows] or None.  The settings are fp32 [rows] (top_k int32) or None."""
+    xd, dev = _act(logits, "logits"), logits.get_device()
+    if logits.dim() != 2:
+        raise ValueError(f"logits: {logits.dim()} dimensions, expected 2")
+    n, V = logits.shape
+    ld = _rows(logits, "logits", (n, V), dev)
+    for t, name, dt in ((u, "u", torch.float32), (token, "token", torch.int32), (prob, "prob", torch.float32),
+                        (temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                        (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+        if t is not None:
+            _want(t, name, dt, (n,), dev)
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        raise ValueError(f"workspace: must be contiguous and on GPU {dev}")
+    _run_on(dev, stream, lib.catq_aux_sample, "catq_aux_sample", logits.data_ptr(), xd, n, V, ld, _ptr(temperature),
+            _ptr(top_k), _ptr(top_p), _ptr(min_p), u.data_ptr(), token.data_ptr(), _ptr(prob), _ptr(workspace),
+            _bytes(workspace))
 
 
 def catq_trace_enable(capacity):

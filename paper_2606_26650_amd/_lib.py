@@ -98,6 +98,8 @@ SIGNATURES = {
     "catq_aux_tree_attention": [PKD, PKC, PKB, PKT, P, F, P, P, P, SZ, P],
     "catq_aux_kv_copy_pages": [PKD, PKC, P, P, I64, P],
     "catq_aux_kv_compact": [PKD, PKC, PKB, P, P, P],
+    "catq_aux_sample_workspace_bytes": [I64, I64],
+    "catq_aux_sample": [P, I32, I64, I64, I64, P, P, P, P, P, P, P, P, SZ, P],
     "catq_aux_rmsnorm_fwd": [P, I32, I64, I64, F, P, P, P],
     "catq_aux_rmsnorm_bwd": [P, I32, P, P, P, I64, I64, P, P],
     "catq_attn_saved_bytes": [PA],
@@ -124,7 +126,7 @@ SIGNATURES = {
 RESTYPES = {"catq_workspace_size": SZ, "catq_status_string": C.c_char_p,
             "catq_last_error_message": C.c_char_p, "catq_attn_saved_bytes": SZ,
             "catq_attn_bwd_workspace_bytes": SZ, "catq_aux_moe_route_workspace_bytes": SZ,
-            "catq_paged_attention_workspace_bytes": SZ,
+            "catq_paged_attention_workspace_bytes": SZ, "catq_aux_sample_workspace_bytes": SZ,
             "catq_trace_pause": None, "catq_trace_reset": None, "catq_trace_disable": None}
 
 _lib = None

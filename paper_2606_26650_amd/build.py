@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libcatq.so")
 
 SOURCES = ["status.hip", "trace.hip", "lmst.hip", "gemm.hip", "linear.hip", "loss.hip", "glue.hip",
            "attention.hip", "flash.hip", "ternary.hip", "ternary_a8.hip", "norm_quant.hip", "kv_cache.hip",
-           "paged_attn.hip", "kv_pages.hip"]
+           "paged_attn.hip", "kv_pages.hip", "sample.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

@@ -1,0 +1,213 @@
+"""Sampling against a plain float64 definition.
+
+A weight is off by at most 2^-23 (the hardware's exp2), 2^-25 of its argument's fraction and 2^-43 of the largest weight,
+so a sum of weights is off by less than 2^-22 of itself and V * 2^-43: DELTA bounds both for V <= 2^20 where a row's
+kept weight is at least the largest one.  The cumulative sums that decide (top-p's, and u's) may fall on either
+side of a border that is that near; the reference is taken with both and the token has to be one of theirs."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DELTA = 2.0 ** -21
+
+
+def _one(x, T, k, p, m, u, dp=0.0, du=0.0):
+    """(token, prob) of one row of float64 logits; dp, du move the borders of top-p and u."""
+    ok = x > -math.inf                                   # (False for NaN)
+    if not ok.any():
+        return -1, 0.0
+    ids = np.flatnonzero(ok)
+    order = ids[np.argsort(-x[ids], kind="stable")]
+    if not T > 0:
+        return int(order[0]), 1.0
+    top = x[order[0]]
+    with np.errstate(invalid="ignore"):
+        w = np.where(x[order] == top, 1.0, np.exp((x[order] - top) / T))
+    if k > 0:
+        order, w = order[:k], w[:k]
+    if p < 1:
+        before = np.concatenate([[0.0], np.cumsum(w)[:-1]])
+        n = max(1, int((before < (p + dp) * w.sum()).sum()))
+        order, w = order[:n], w[:n]
+    if m > 0:
+        n = max(1, int((w >= m).sum()))
+        order, w = order[:n], w[:n]
+    by_id = np.argsort(order)
+    order, w = order[by_id], w[by_id]
+    cum = np.cumsum(w)
+    u = 0.0 if not u > 0 else min(u, 1 - 2.0 ** -24)
+    at = min(int((cum <= (u + du) * cum[-1]).sum()), len(order) - 1)
+    return int(order[at]), float(w[at] / cum[-1])
+
+
+def _check(catq, logits, u, T=None, k=None, p=None, m=None, ld=None, repeat=True):
+    n, V = logits.shape
+    if ld is None:
+        dev = logits.cuda()
+    else:
+        wide = torch.full((n, ld), 1e4, dtype=logits.dtype, device="cuda")     # (what lies between the rows is large)
+        wide[:, :V] = logits.cuda()
+        dev = wide[:, :V]
+    f = lambda v, dt=torch.float32: None if v is None else torch.tensor(v, dtype=dt, device="cuda")  # noqa: E731
+    args = dict(temperature=f(T), top_k=f(k, torch.int32), top_p=f(p), min_p=f(m))
+    token = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    prob = torch.full((n,), -7.0, device="cuda")
+    ws = torch.empty(max(16, catq.catq_aux_sample_workspace_bytes(n, V)), dtype=torch.uint8, device="cuda")
+    ws.fill_(255)
+    catq.catq_aux_sample(dev, f(u), token, ws, prob=prob, **args)
+    x = logits.double().numpy()
+    u32 = np.asarray(u, dtype=np.float32).astype(float)
+    for r in range(n):
+        row = [np.float32(v[r]).astype(float) if v is not None else d for v, d in ((T, 1.0), (p, 1.0), (m, 0.0))]
+        kk = 0 if k is None else k[r]
+        want = {_one(x[r], row[0], kk, row[1], row[2], u32[r], dp, du) for dp in (0.0, -DELTA, DELTA)
+                for du in (0.0, -DELTA, DELTA)}
+        got = int(token[r]), float(prob[r])
+        near = [q for t, q in want if t == got[0]]
+        assert near, (r, got, want, [None if v is None else v[r] for v in (T, k, p, m)], u[r])
+        assert min(abs(got[1] - q) for q in near) <= DELTA * got[1] + 1e-30, (r, got, want)
+    if repeat:
+        again = torch.empty_like(token)
+        catq.catq_aux_sample(dev, f(u), again, ws, **args)
+        assert torch.equal(again, token)
+    return token, prob
+
+
+def _gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+SIZES = [(1, 1, None), (3, 2, None), (5, 7, 9), (4, 100, None), (6, 1000, 1003), (3, 4097, None), (8, 32000, None),
+         (5, 50257, 50261), (4, 150000, None), (1, 262147, None), (70, 300, 301), (2, 1 << 20, None)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,ld", SIZES)
+def test_sample(catq, rows, V, ld, dtype):
+    g = _gen(V + rows)
+    x = (torch.randn((rows, V), generator=g) * 2.5).to(dtype)
+    x[:, ::max(1, V // 9)] += 5
+    r = np.random.RandomState(V)
+    for settings in range(7):
+        on = [[0, 0, 0], [1, 0, 0], [0, 1, 0], [0, 0, 1], [1, 1, 0], [0, 1, 1], [1, 1, 1]][settings]
+        _check(catq, x, r.rand(rows), T=r.uniform(0.3, 1.5, rows),
+               k=[int(v) for v in r.choice([1, 2, 40, 400, 5000, 2 ** 31 - 1], rows)] if on[0] else None,
+               p=r.uniform(0.05, 0.999, rows) if on[1] else None, m=r.uniform(0.001, 0.3, rows) if on[2] else None,
+               ld=ld, repeat=settings == 6)
+
+
+def test_sample_ties(catq):
+    """Equal logits by the hundred thousand: the filters end inside them, by index; and in every place of the row."""
+    V = 100003
+    g = _gen(1)
+    x = torch.zeros((9, V))
+    x[1] = torch.randint(0, 3, (V,), generator=g).float()
+    x[2] = -3.0
+    x[2, V - 1] = 4.0
+    x[3, :50000] = 1.0
+    x[4] = torch.randint(0, 2, (V,), generator=g).float() * 1e-30        # different keys, one bin
+    x[5] = 1.0 + torch.randint(0, 100000, (V,), generator=g).float() * 2.0 ** -23
+    x[6] = torch.where(torch.rand(V, generator=g) < 0.5, 0.0, -0.0)        # the same logit
+    x[7, ::2] = -math.inf
+    x[8, 1:] = -40.0                                                       # the others weigh nothing
+    for dtype in (torch.float32, torch.bfloat16):
+        for k, p in ((None, None), (30000, None), (None, 0.37), (70001, 0.61), (7, 0.5), (2049, 0.999), (1, 0.3)):
+            _check(catq, x.to(dtype), [0.0, 0.3, 0.5, 0.9, 0.123, 0.77, 0.999, 0.2, 0.4], T=[1.0, 0.7, 2.0] * 3,
+                   k=None if k is None else [k] * 9, p=None if p is None else [p] * 9)
+
+
+def test_sample_kept_sets(catq):
+    """Over all u, exactly the kept tokens come out."""
+    V, n = 50, 4000
+    g = _gen(2)
+    row = torch.randn(V, generator=g) * 2
+    u = (np.arange(n) + 0.5) / n
+    order = torch.argsort(row, descending=True, stable=True).tolist()
+    w = torch.softmax(row.double(), 0)
+    for k, p, m in ((3, 1.0, 0.0), (0, 0.8, 0.0), (0, 1.0, 0.1), (10, 0.9, 0.05), (0, 1e-9, 0.0), (0, 1.0, 1.0)):
+        token, _ = _check(catq, row.expand(n, V).contiguous(), u, T=[1.0] * n, k=[k] * n, p=[p] * n, m=[m] * n,
+                          repeat=False)
+        ws = w[order[:k or V]]
+        before = ws.cumsum(0) - ws
+        keep = [t for j, t in enumerate(order[:k or V])
+                if j == 0 or (before[j] < np.float32(p) * ws.sum() and w[t] >= np.float32(m) * w[order[0]])]
+        share = {t: float(w[t] / w[keep].sum()) for t in keep}
+        counts = torch.bincount(token.cpu(), minlength=V)
+        for t in range(V):
+            assert abs(int(counts[t]) - share.get(t, 0.0) * n) <= 2, (t, k, p, m)
+
+
+def test_sample_odd_rows(catq):
+    V = 3001
+    inf, nan = math.inf, math.nan
+    g = _gen(3)
+    x = torch.randn((14, V), generator=g)
+    x[0] = -inf
+    x[1] = nan
+    x[2] = -inf
+    x[2, 77] = -3e38                          # one token is left
+    x[3, 5], x[3, 2000], x[3, 2999] = inf, inf, inf
+    x[4, 9] = nan
+    x[5, ::3] = nan
+    x[6] = -inf
+    x[6, 3000], x[6, 0] = 1.0, 1.0
+    x[7] = x[7] * 1e38
+    x[8] = 3.0e38
+    x[8, 4] = -3.0e38
+    for u in (0.0, 0.34, 0.67, 0.9999999):
+        token, prob = _check(catq, x, [u] * 14)
+        assert token[:2].tolist() == [-1, -1] and prob[:2].tolist() == [0.0, 0.0] and int(token[2]) == 77
+        assert int(token[3]) in (5, 2000, 2999)
+        _check(catq, x, [u] * 14, k=[5] * 14, p=[0.9] * 14, m=[0.01] * 14)
+        # settings at and past their ends
+        one = [0.0, -1.0, nan, inf, 1e-30, 1e30, 1e-45, 3e38, 1.0, 1.0, 1.0, 1.0, 1.0, 1.0]
+        _check(catq, x[9:10].expand(14, V).contiguous(), [u] * 14, T=one, k=[50] * 14, p=[0.95] * 14)
+        _check(catq, x[9:10].expand(14, V).contiguous(), [u] * 14, k=[-1, 0, 1, V, V + 1, 2 ** 31 - 1, -2 ** 31] * 2,
+               p=[1.0, 2.0, inf, nan, -inf, 0.0, -1.0] + [0.5] * 7, m=[0.0, -1.0, nan, 1.0, 2.0, inf, 0.2] * 2)
+    bad = [nan, -1.0, inf, 1.0, 1.5, -inf, 1 - 2.0 ** -24] * 2
+    token, _ = _check(catq, x[9:10].expand(14, V).contiguous(), bad, repeat=False)
+    assert int(token[0]) == int(token[1]) == int(token[5]) and int(token[2]) == int(token[3]) == int(token[4])
+
+
+def test_sample_captured_and_on_another_stream(catq):
+    g = _gen(4)
+    V = 120000
+    x = (torch.randn((3, 5, V), generator=g) * 2).cuda()
+    u = torch.rand((3, 5), generator=g).cuda()
+    logits, uu = torch.empty((5, V), device="cuda"), torch.empty(5, device="cuda")
+    token, prob = torch.empty(5, dtype=torch.int32, device="cuda"), torch.empty(5, device="cuda")
+    ws = torch.empty(max(16, catq.catq_aux_sample_workspace_bytes(5, V)), dtype=torch.uint8, device="cuda")
+    top_k = torch.tensor([0, 50, 0, 5000, 0], dtype=torch.int32, device="cuda")
+    top_p = torch.tensor([0.9, 1.0, 1.0, 0.99, 0.5], device="cuda")
+
+    def step(stream=None):
+        catq.catq_aux_sample(logits, uu, token, ws, top_k=top_k, top_p=top_p, prob=prob, stream=stream)
+
+    want = []
+    for i in range(3):
+        logits.copy_(x[i])
+        uu.copy_(u[i])
+        step()
+        want.append((token.clone(), prob.clone()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in (0, 1, 2, 1):
+        logits.copy_(x[i])
+        uu.copy_(u[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(token, want[i][0]) and torch.equal(prob, want[i][1])
+    side = torch.cuda.Stream()
+    logits.copy_(x[0])
+    uu.copy_(u[0])
+    side.wait_stream(torch.cuda.current_stream())
+    step(side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(token, want[0][0]) and torch.equal(prob, want[0][1])
