@@ -307,6 +307,37 @@ catq_status catq_ternary_linear_a8(const int8_t* q, int64_t M, int64_t ldq, cons
                                    int64_t d_in, int32_t g, void* Y, catq_dtype y_dtype,
                                    int64_t ldy, hipStream_t stream);
 
+/* catq_ternary_moe_a8 -- a layer of routed experts on that storage and 8-bit activations, from the router's
+ * logits to the combined output, for few tokens:
+ *   e_1 .. e_k, w_1 .. w_k   the top_k largest logits of a token and their softmax, as catq_aux_moe_route has them
+ *                            (ties, NaN and -inf too)
+ *   [gate | up]_j = x_scale * q (gu_alpha T)^T of expert e_j,   a_j = silu(gate_j) * up_j   (fp32)
+ *   qa_j, s_j     = the codes and the one scale of a_j, as catq_aux_act_quant8 has them
+ *   y             = res + sum_j w_j * s_j * qa_j (down_alpha T)^T of expert e_j
+ * Inner sums are exact integers, the others fp32 in a fixed order (bitwise deterministic for a given
+ * shape and routing); what one token or expert holds does not reach the tokens without it.
+ *   logits      fp32 [T][n_experts]
+ *   q, ldq      int8 [T][ldq] codes with one scale per token, x_scale fp32 [T], as for catq_ternary_linear_a8
+ *   gu_packed   uint8 [n_experts][2 ffn][hidden/4] (gate rows, then up rows), gu_alpha fp32 [n_experts][2 ffn]
+ *               [hidden/group_size]
+ *   down_packed uint8 [n_experts][hidden][ffn/4], down_alpha fp32 [n_experts][hidden][ffn/group_size]
+ *   res, y      [T][hidden] of y_dtype (fp32 or bf16); res may be NULL, or y
+ *   workspace   at least catq_ternary_moe_a8_workspace_bytes(d, T) bytes, for one call at a time
+ * T <= 1024 (0 is a no-op); the weights are read once for each 16 tokens that hit an expert, so from some 100 tokens
+ * on the grouped rows of catq_aux_moe_gather are the better order.  logits and x_scale 4-byte aligned, the others
+ * 16-byte. */
+typedef struct {
+  int32_t n_experts, top_k;   /* at most 1024, and 16                                     */
+  int32_t hidden, ffn;        /* multiples of group_size, at most 32768                   */
+  int32_t group_size;         /* of the weights: 128 times a power of two                 */
+} catq_moe_desc;
+size_t catq_ternary_moe_a8_workspace_bytes(const catq_moe_desc* d, int64_t T);
+catq_status catq_ternary_moe_a8(const catq_moe_desc* d, const float* logits, const int8_t* q, int64_t T,
+                                int64_t ldq, const float* x_scale, const uint8_t* gu_packed,
+                                const float* gu_alpha, const uint8_t* down_packed, const float* down_alpha,
+                                const void* res, void* y, catq_dtype y_dtype, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+
 /* Fused variants for the SwiGLU MLP of a decoder block (a4 and a8 with the
  * SwiGLU of a5 / a7 in the GEMM epilogue; same results as the unfused calls).
  *

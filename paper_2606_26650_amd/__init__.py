@@ -12,7 +12,8 @@ import torch
 
 from . import _lib
 from ._lib import (BF16, F32, HARD, IDENTITY, SOFT, WS_LINEAR_BWD, WS_LOSS, AttnDesc, CatqError,
-                   KvBatch, KvCache, KvDesc, KvPrep, KvTree, LmstParams)
+                   KvBatch, KvCache, KvDesc, KvPrep, KvTree, LmstParams,
+                   MoeDesc)
 
 __all__ = [
     "catq_modulate_ternarize", "catq_fakeq_linear_fwd", "catq_fakeq_linear_bwd",
@@ -27,7 +28,8 @@ __all__ = [
     "catq_ternary_linear_a8", "catq_aux_rmsnorm_quant", "catq_aux_act_quant8", "catq_aux_kv_append",
     "catq_aux_kv_read", "catq_aux_paged_attention", "catq_paged_attention_workspace_bytes",
     "catq_aux_kv_append_tree", "catq_aux_tree_attention", "catq_aux_kv_copy_pages", "catq_aux_kv_compact",
-    "catq_aux_sample", "catq_aux_sample_workspace_bytes",
+    "catq_aux_sample", "catq_aux_sample_workspace_bytes", "catq_ternary_moe_a8",
+    "catq_ternary_moe_a8_workspace_bytes", "moe_desc", "MoeDesc",
     "kv_desc", "kv_cache", "kv_batch", "kv_prep", "kv_tree", "KvDesc", "KvCache", "KvBatch", "KvPrep", "KvTree",
     "lmst_params", "attn_desc", "IDENTITY", "SOFT", "HARD", "F32", "BF16", "CatqError",
     "LmstParams", "AttnDesc", "lib", "catq_trace_enable", "catq_trace_pause",
@@ -429,6 +431,43 @@ def catq_ternary_linear_a8(q, x_scale, packed, alpha, Y, g=128, stream=None):
     _per_group(alpha, "alpha", d_out, d_in, g, dev)
     _run_on(dev, stream, lib.catq_ternary_linear_a8, "catq_ternary_linear_a8", q.data_ptr(), M, ldq,
             x_scale.data_ptr(), packed.data_ptr(), alpha.data_ptr(), d_out, d_in, g, Y.data_ptr(), yd, ldy)
+
+
+def moe_desc(n_experts, top_k, hidden, ffn, group_size=128):
+    """Geometry of a layer of routed experts on packed weights (see catq_moe_desc in the header)."""
+    _int32(n_experts=n_experts, top_k=top_k, hidden=hidden, ffn=ffn, group_size=group_size)
+    return MoeDesc(n_experts, top_k, hidden, ffn, group_size)
+
+
+def catq_ternary_moe_a8_workspace_bytes(desc, T):
+    return int(lib.catq_ternary_moe_a8_workspace_bytes(C.byref(desc), T))
+
+
+def catq_ternary_moe_a8(desc, logits, q, x_scale, gu_packed, gu_alpha, down_packed, down_alpha, y, workspace,
+                        res=None, stream=None):
+    """y = res + the routed experts' output of few tokens: logits fp32 [T][E], codes q int8 [T][hidden] (rows may be
+    strided) with x_scale fp32 [T], gu_packed uint8 [E][2 ffn][hidden/4], down_packed uint8 [E][hidden][ffn/4] and
+    their scales, y (and res) fp32 or bf16 [T][hidden]."""
+    d, dev, T = desc, logits.get_device(), logits.shape[0]
+    E, h, F, g = d.n_experts, d.hidden, d.ffn, max(d.group_size, 1)
+    _want(logits, "logits", torch.float32, (T, E), dev)
+    if q.dtype is not torch.int8:
+        raise TypeError(f"q: dtype {q.dtype}, expected torch.int8")
+    ldq = _rows(q, "q", (T, h), dev)
+    _want(x_scale, "x_scale", torch.float32, (T,), dev)
+    _want(gu_packed, "gu_packed", torch.uint8, (E, 2 * F, h // 4), dev)
+    _want(gu_alpha, "gu_alpha", torch.float32, (E, 2 * F, h // g), dev)
+    _want(down_packed, "down_packed", torch.uint8, (E, h, F // 4), dev)
+    _want(down_alpha, "down_alpha", torch.float32, (E, h, F // g), dev)
+    yd = _act(y, "y")
+    _want(y, "y", y.dtype, (T, h), dev)
+    if res is not None:
+        _want(res, "res", y.dtype, (T, h), dev)
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace: must be contiguous and on GPU {dev}")
+    _run_on(dev, stream, lib.catq_ternary_moe_a8, "catq_ternary_moe_a8", C.byref(d), logits.data_ptr(), q.data_ptr(), T,
+            ldq, x_scale.data_ptr(), gu_packed.data_ptr(), gu_alpha.data_ptr(), down_packed.data_ptr(),
+            down_alpha.data_ptr(), _ptr(res), y.data_ptr(), yd, workspace.data_ptr(), _bytes(workspace))
 
 
 def _int32(**sizes):

@@ -55,6 +55,10 @@ class KvTree(C.Structure):
     _fields_ = [("mask", C.c_void_p), ("depth", C.c_void_p), ("words", C.c_int32)]
 
 
+class MoeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_experts", "top_k", "hidden", "ffn", "group_size")]
+
+
 class TraceRec(C.Structure):
     _fields_ = [("tag", C.c_char * 96), ("flops", C.c_double), ("bytes", C.c_double),
                 ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("ms", C.c_float)]
@@ -69,6 +73,7 @@ class CatqError(RuntimeError):
 P, I64, I32, F, SZ = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_size_t
 PP = C.POINTER(LmstParams)
 PA = C.POINTER(AttnDesc)
+PMD = C.POINTER(MoeDesc)
 PKD, PKC, PKB, PKP, PKT = (C.POINTER(s) for s in (KvDesc, KvCache, KvBatch, KvPrep, KvTree))
 
 SIGNATURES = {
@@ -84,6 +89,8 @@ SIGNATURES = {
     "catq_fakeq_down_swiglu_bwd": [P, P, I64, I64, I64, P, P, P, P],
     "catq_ternary_linear": [P, I64, I64, P, P, I64, I64, I32, P, I32, I64, P],
     "catq_ternary_linear_a8": [P, I64, I64, P, P, P, I64, I64, I32, P, I32, I64, P],
+    "catq_ternary_moe_a8_workspace_bytes": [PMD, I64],
+    "catq_ternary_moe_a8": [PMD, P, P, I64, I64, P, P, P, P, P, P, P, I32, P, SZ, P],
     "catq_workspace_size": [I32, I64, I64, I64, I32],
     "catq_status_string": [I32],
     "catq_last_error_message": [],
@@ -127,6 +134,7 @@ RESTYPES = {"catq_workspace_size": SZ, "catq_status_string": C.c_char_p,
             "catq_last_error_message": C.c_char_p, "catq_attn_saved_bytes": SZ,
             "catq_attn_bwd_workspace_bytes": SZ, "catq_aux_moe_route_workspace_bytes": SZ,
             "catq_paged_attention_workspace_bytes": SZ, "catq_aux_sample_workspace_bytes": SZ,
+            "catq_ternary_moe_a8_workspace_bytes": SZ,
             "catq_trace_pause": None, "catq_trace_reset": None, "catq_trace_disable": None}
 
 _lib = None

@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libcatq.so")
 
 SOURCES = ["status.hip", "trace.hip", "lmst.hip", "gemm.hip", "linear.hip", "loss.hip", "glue.hip",
            "attention.hip", "flash.hip", "ternary.hip", "ternary_a8.hip", "norm_quant.hip", "kv_cache.hip",
-           "paged_attn.hip", "kv_pages.hip", "sample.hip"]
+           "paged_attn.hip", "kv_pages.hip", "sample.hip", "moe_a8.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
@@ -32,7 +32,8 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
 # matrix-core accumulators in ordinary VGPRs (they scale them after every
 # 128-code chunk, so accumulation registers would cost a copy each time)
 EXTRA = {"ternary.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "ternary_a8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "ternary_a8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "moe_a8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> str:
