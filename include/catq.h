@@ -619,7 +619,7 @@ catq_status catq_aux_kv_compact(const catq_kv_desc* d, const catq_kv_cache* cach
                                 hipStream_t stream);
 
 /*
- * catq_aux_sample: a token for each row of logits [rows][ld] (fp32 or bf16; V of them, V <= 2^20, ld >= V).
+ * catq_aux_sample: a token for each row of logits [rows][ld] (fp32 or bf16; V of them, V <= 2^20, ld >= V, rows <= 65535).
  * Tokens are ordered by logit, the largest first, equal ones by index, and weigh
  * w = exp((logit - largest) / temperature).  Kept are, one filter after the other,
  *   top_k   the first top_k tokens (<= 0: all)

@@ -8,7 +8,17 @@
 // Weights.  w = exp((logit - largest) / temperature) as an integer multiple of 2^-43: the exponent is taken in fp64
 // (far tokens and small temperatures lose nothing), its fraction through the hardware's exp2 in fp32, off by one unit
 // of 2^-23.  Sums of at most 2^20 weights of at most 1 are exact in 64 bits and do not depend on their order, so
-// atomics in LDS give the same result every time.
+// atomics give the same result every time.
+//
+// Steps.  A row's tokens go into 2048 bins of 1/64 of exp's argument below the largest logit, with their number and
+// their weight.  The bins tell where top-k (or, without it, top-p) ends.  Where the tokens up to that bin are few, they
+// are gathered and the rest happens in LDS; where they are many, that bin's tokens are, and the weight before it is summed
+// by slices of the row, of which the one where u falls is read again.  Only the bins in which a filter ends are sorted.
+// Without top-k and top-p no bins are needed, only the weight of every slice.
+//
+// Rows of more than kAlone tokens are read by several workgroups each: the largest logit of every slice, then bins
+// or weights of every slice, then the gathering, then one workgroup a row for what is left.
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -18,10 +28,24 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kT = 1024;              // threads of a workgroup
+constexpr int kT = 1024;              // threads of the workgroup that picks a row's token
+constexpr int kS = 256;               // threads of one that reads a slice
 constexpr int kBins = 2048;
-constexpr int kList = 2048;           // composites that are sorted in LDS
+constexpr int kList = 4096;           // composites that are gathered
+constexpr int kSort = 1024;           // that are sorted
 constexpr int kOne = 43;              // a weight of 1 is 2^43
+constexpr int kMaxSlices = 256;
+
+// What the workgroups of a row leave for those after them
+struct RowSpace {
+  u64 first[kMaxSlices];              // slice: its first composite
+  u64 mass[kMaxSlices];               // slice: the weight that it keeps (rows without top-k and top-p)
+  u64 bin_mass[kBins];
+  u64 list[kList];
+  unsigned int bin_count[kBins];
+  unsigned int n;                     // composites in the list
+  unsigned int pad[3];
+};
 
 struct SampleArgs {
   const void* logits;
@@ -34,7 +58,28 @@ struct SampleArgs {
   const float* u;
   int32_t* token;
   float* prob;
+  RowSpace* space;      // [rows], where a row has several workgroups
+  int32_t slices;       // of a row
+  int32_t slice;        // tokens of a slice
 };
+
+// A row's settings
+struct Settings {
+  float temp, top_p, min_p;
+  int top_k;
+  bool first_only;      // the first token is taken
+  bool filtered;        // top-k or top-p
+};
+__device__ __forceinline__ Settings settings(const SampleArgs& a, int64_t row) {
+  Settings p;
+  p.temp = a.temperature ? a.temperature[row] : 1.0f;
+  p.top_p = a.top_p ? a.top_p[row] : 1.0f;
+  p.min_p = a.min_p ? a.min_p[row] : 0.0f;
+  p.top_k = a.top_k ? a.top_k[row] : 0;
+  p.first_only = !(p.temp > 0.0f) || p.top_k == 1 || p.top_p <= 0.0f;
+  p.filtered = p.top_k > 0 || p.top_p < 1.0f;
+  return p;
+}
 
 __device__ __forceinline__ unsigned int key_of(float x) {
   const unsigned int u = x == 0.0f ? 0u : __float_as_uint(x);   // (-0 as 0)
@@ -50,11 +95,25 @@ __device__ __forceinline__ float logit_of(u64 c) {
 struct Row {
   float top;       // its largest logit
   double scale;    // log2(e) / temperature
+  double offset;   // -top * scale
   float bins;      // bins per unit of logit
 };
-// (logit - largest) log2(e) / temperature; equal ones give 0 also where both are infinite
+__device__ __forceinline__ Row row_of(u64 first, float temp) {
+  Row r;
+  r.top = logit_of(first);
+  r.scale = 1.4426950408889634 / (double)temp;
+  r.offset = -(double)r.top * r.scale;
+  r.bins = fminf(64.0f / temp, 1e30f);
+  return r;
+}
+// the least exponent that min-p keeps
+__device__ __forceinline__ double least_of(float min_p) {
+  return min_p > 0.0f ? fmin(log2((double)min_p), 0.0) : -INFINITY;
+}
+// (logit - largest) log2(e) / temperature, off by 2^-53 of the larger product; equal ones give 0 also where both
+// are infinite
 __device__ __forceinline__ double exponent(const Row& r, float x) {
-  return x == r.top ? 0.0 : ((double)x - (double)r.top) * r.scale;
+  return x == r.top ? 0.0 : fma((double)x, r.scale, r.offset);
 }
 __device__ __forceinline__ u64 weight(const Row& r, float x) {
   const double z = exponent(r, x);
@@ -95,19 +154,20 @@ __device__ __forceinline__ void for_range(const T* row, int V, int i0, int i1, i
         }
       }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
+    // one piece at a time, the others moved up: the code is there once
+#pragma unroll 1
+    for (int u = 0; u < U && v + u * lanes <= v1; ++u) {
       const int e0 = (v + u * lanes) * E - off;
-      if (v + u * lanes > v1) continue;
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         const int i = e0 + j;
-        if (i < i0 || i >= i1) continue;
         float x;
-        if constexpr (sizeof(T) == 4) x = __uint_as_float(raw[u][j]);
-        else x = (j & 1) ? bf16_hi(raw[u][j / 2]) : bf16_lo(raw[u][j / 2]);
-        if (x > -INFINITY) f(x, i);    // (not -inf, no NaN)
+        if constexpr (sizeof(T) == 4) x = __uint_as_float(raw[0][j]);
+        else x = (j & 1) ? bf16_hi(raw[0][j / 2]) : bf16_lo(raw[0][j / 2]);
+        if (x > -INFINITY && (unsigned)(i - i0) < (unsigned)(i1 - i0)) f(x, i);    // (not -inf, no NaN)
       }
+#pragma unroll
+      for (int w = 0; w + 1 < U; ++w) raw[w] = raw[w + 1];
     }
   }
 }
@@ -115,6 +175,7 @@ __device__ __forceinline__ void for_range(const T* row, int V, int i0, int i1, i
 __device__ __forceinline__ u64 shfl_up64(u64 v, int d) { return __shfl_up(v, d, 64); }
 
 // Inclusive prefix sum over the workgroup; `total` is the whole.  s: one value per wave.
+template <int NT>
 __device__ __forceinline__ u64 block_scan(u64 v, u64* s, u64& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -128,14 +189,14 @@ __device__ __forceinline__ u64 block_scan(u64 v, u64* s, u64& total) {
   u64 before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kT / 64; ++w) {
+  for (int w = 0; w < NT / 64; ++w) {
     const u64 t = s[w];
     if (w < wave) before += t;
     total += t;
   }
   return v + before;
 }
-template <typename F>
+template <int NT, typename F>
 __device__ __forceinline__ u64 block_reduce(u64 v, u64* s, F&& f) {
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) v = f(v, (u64)__shfl_xor(v, d, 64));
@@ -144,78 +205,145 @@ __device__ __forceinline__ u64 block_reduce(u64 v, u64* s, F&& f) {
   __syncthreads();
   v = s[0];
 #pragma unroll
-  for (int w = 1; w < kT / 64; ++w) v = f(v, s[w]);
+  for (int w = 1; w < NT / 64; ++w) v = f(v, s[w]);
   return v;
+}
+template <int NT>
+__device__ __forceinline__ u64 block_min(u64 v, u64* s) {
+  return block_reduce<NT>(v, s, [](u64 p, u64 q) { return min(p, q); });
+}
+
+// Where the filters end among the bins: top-k, if it leaves a token out, or else top-p.
+struct Ends {
+  u64 n_all, m_all;      // the row's tokens and weight
+  bool by_k, both;       // top-k ends there; top-p is still to come
+  int last;              // the bin of the last token, kBins where all are kept
+  u64 want, base;        // (top-k) that token's place in the bin; the weight before the bin
+  u64 in_bin, count;     // tokens of the bin, and up to it
+};
+// What is gathered: all tokens up to the last bin; where they are too many, the last bin's alone; nothing where these
+// are too many too, or where top-p ends somewhere before top-k.
+enum { kGatherAll, kGatherBin, kGatherNone };
+__device__ __forceinline__ int gathered(const Ends& e) {
+  return e.count <= kList ? kGatherAll : !e.both && e.in_bin <= kList ? kGatherBin : kGatherNone;
+}
+// at: eight values in LDS
+template <int NT>
+__device__ __forceinline__ Ends find_ends(const unsigned int* count, const u64* mass, int top_k, float top_p, u64* s,
+                                          u64* at) {
+  constexpr int B = kBins / NT;
+  const int t = B * threadIdx.x;
+  unsigned int c[B];
+  u64 m[B], cs = 0, ms = 0;
+#pragma unroll
+  for (int i = 0; i < B; ++i) {
+    c[i] = count[t + i];
+    m[i] = mass[t + i];
+    cs += c[i];
+    ms += m[i];
+  }
+  Ends e;
+  const u64 pc = block_scan<NT>(cs, s, e.n_all) - cs, pm = block_scan<NT>(ms, s, e.m_all) - ms;
+  const bool by_k = top_k > 0 && (u64)top_k < e.n_all;
+  const double target = (double)top_p * (double)e.m_all;
+  u64 ec = pc, em = pm;
+#pragma unroll
+  for (int i = 0; i < B; ++i) {
+    const bool here = by_k ? ec < (u64)top_k && (u64)top_k <= ec + c[i]
+                           : top_p < 1.0f && (double)em < target && target <= (double)(em + m[i]);
+    if (here) {
+      at[0] = t + i;
+      at[1] = (u64)top_k - ec;
+      at[2] = em;
+      at[3] = c[i];
+      at[4] = ec + c[i];
+    }
+    ec += c[i];
+    em += m[i];
+  }
+  __syncthreads();
+  const bool some = by_k || top_p < 1.0f;
+  e.by_k = by_k;
+  e.both = by_k && top_p < 1.0f;
+  e.last = some ? (int)at[0] : kBins;
+  e.want = at[1];
+  e.base = some ? at[2] : e.m_all;
+  e.in_bin = some ? at[3] : 0;
+  e.count = some ? at[4] : e.n_all;
+  __syncthreads();
+  return e;
 }
 
 struct Shared {
-  u64 list[kList];
-  u64 mass[kBins];
+  u64 list[kList];      // what has been gathered
+  u64 sort[kSort];      // of one bin, in order
+  u64 mass[kBins];      // the row's bins
+  u64 part_mass[kBins];
   unsigned int count[kBins];
+  unsigned int part_count[kBins];
   u64 wave[kT / 64];
-  u64 at[4];
+  u64 at[8];
   unsigned int n;
 };
 
-// s.list[0 .. n) in ascending order (n <= kList)
+// s.sort[0 .. n) in ascending order (n <= kSort)
 __device__ __forceinline__ void sort_list(Shared& s, int n) {
   int size = 2;
   while (size < n) size <<= 1;
-  for (int i = n + threadIdx.x; i < size; i += kT) s.list[i] = ~0ull;
+  if (n + (int)threadIdx.x < size) s.sort[n + threadIdx.x] = ~0ull;
   __syncthreads();
   for (int k = 2; k <= size; k <<= 1)
     for (int j = k >> 1; j > 0; j >>= 1) {
-      for (int p = threadIdx.x; p < size / 2; p += kT) {
+      const int p = threadIdx.x;
+      if (p < size / 2) {
         const int a = 2 * (p & ~(j - 1)) + (p & (j - 1)), b = a + j;
-        const u64 x = s.list[a], y = s.list[b];
+        const u64 x = s.sort[a], y = s.sort[b];
         if ((x > y) == ((a & k) == 0)) {
-          s.list[a] = y;
-          s.list[b] = x;
+          s.sort[a] = y;
+          s.sort[b] = x;
         }
       }
       __syncthreads();
     }
 }
 
-// Of the row's tokens in bin b (n of them): the composite of the last one that is kept, and their mass up to it.
+// Of the tokens in bin b (n of them): the composite of the last one that is kept, and their mass up to it.
 // By count: the first `want` of them are kept.  By mass: those before which the mass (with `base`) is below `target`,
-// of the ones with c <= most.
+// of the ones with c <= most.  each(f) calls f(logit, composite) for every token of the row that may be in the bin.
 struct Bound {
   u64 c, mass;
 };
-template <typename T>
-__device__ Bound resolve(Shared& s, const T* row, int V, const Row& r, int b, int n, bool by_mass, u64 want, u64 base,
-                         double target, u64 most) {
+template <typename Each>
+__device__ __forceinline__ Bound resolve(Shared& s, Each&& each, const Row& r, int b, int n, bool by_mass, u64 want,
+                                         u64 base, double target, u64 most) {
   u64 lo = 0, hi = most, before = 0;      // composites lo .. hi are in question; the mass of those below lo
-  // more than the list takes: the interval is cut to one of up to 2048 parts, again and again
-  while (n > kList) {
+  // more than are sorted: the interval is cut to one of up to 2048 parts, again and again
+  while (n > kSort) {
     u64 least = ~0ull, last = 0;
-    for_range<T>(row, V, 0, V, threadIdx.x, kT, [&](float x, int i) {
-      const u64 c = composite(x, i);
+    each([&](float x, u64 c) {
       if (bin_of(r, x) != b || c < lo || c > hi) return;
       least = min(least, c);
       last = max(last, c);
     });
-    lo = block_reduce(least, s.wave, [](u64 p, u64 q) { return min(p, q); });
-    hi = block_reduce(last, s.wave, [](u64 p, u64 q) { return max(p, q); });
+    lo = block_min<kT>(least, s.wave);
+    hi = block_reduce<kT>(last, s.wave, [](u64 p, u64 q) { return max(p, q); });
     const int bits = 64 - __builtin_clzll((hi - lo) | 1);
     const int shift = bits > 11 ? bits - 11 : 0;
     for (int i = threadIdx.x; i < kBins; i += kT) {
-      s.count[i] = 0;
-      s.mass[i] = 0;
+      s.part_count[i] = 0;
+      s.part_mass[i] = 0;
     }
     __syncthreads();
-    for_range<T>(row, V, 0, V, threadIdx.x, kT, [&](float x, int i) {
-      const u64 c = composite(x, i);
+    each([&](float x, u64 c) {
       if (bin_of(r, x) != b || c < lo || c > hi) return;
-      atomicAdd(&s.count[(c - lo) >> shift], 1u);
-      atomicAdd(&s.mass[(c - lo) >> shift], weight(r, x));
+      atomicAdd(&s.part_count[(c - lo) >> shift], 1u);
+      atomicAdd(&s.part_mass[(c - lo) >> shift], weight(r, x));
     });
     __syncthreads();
     const int t = 2 * threadIdx.x;
     u64 all;
-    const u64 c0 = s.count[t], c1 = s.count[t + 1], m0 = s.mass[t], m1 = s.mass[t + 1];
-    const u64 pc = block_scan(c0 + c1, s.wave, all) - c0 - c1, pm = block_scan(m0 + m1, s.wave, all) - m0 - m1;
+    const u64 c0 = s.part_count[t], c1 = s.part_count[t + 1], m0 = s.part_mass[t], m1 = s.part_mass[t + 1];
+    const u64 pc = block_scan<kT>(c0 + c1, s.wave, all) - c0 - c1, pm = block_scan<kT>(m0 + m1, s.wave, all) - m0 - m1;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const u64 ec = pc + (k ? c0 : 0), em = pm + (k ? m0 : 0), c = k ? c1 : c0, m = k ? m1 : m0;
@@ -239,29 +367,21 @@ __device__ Bound resolve(Shared& s, const T* row, int V, const Row& r, int b, in
   }
   if (threadIdx.x == 0) s.n = 0;
   __syncthreads();
-  for_range<T>(row, V, 0, V, threadIdx.x, kT, [&](float x, int i) {
-    const u64 c = composite(x, i);
+  each([&](float x, u64 c) {
     if (bin_of(r, x) != b || c < lo || c > hi) return;
     const unsigned int at = atomicAdd(&s.n, 1u);
-    if (at < kList) s.list[at] = c;
+    if (at < kSort) s.sort[at] = c;
   });
   __syncthreads();
-  n = (int)min(s.n, (unsigned)kList);
+  n = (int)min(s.n, (unsigned)kSort);
   sort_list(s, n);
-  // two neighbours a thread
-  const int t = 2 * threadIdx.x;
-  const u64 m0 = t < n ? weight(r, logit_of(s.list[t])) : 0, m1 = t + 1 < n ? weight(r, logit_of(s.list[t + 1])) : 0;
+  const int t = threadIdx.x;
+  const u64 m = t < n ? weight(r, logit_of(s.sort[t])) : 0;
   u64 all;
-  const u64 pm = block_scan(m0 + m1, s.wave, all) - m0 - m1;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const u64 em = before + pm + (k ? m0 : 0), m = k ? m1 : m0;
-    const bool here = t + k < n && (by_mass ? (double)(base + em) < target && target <= (double)(base + em + m)
-                                            : (u64)(t + k + 1) == want);
-    if (here) {
-      s.at[0] = s.list[t + k];
-      s.at[1] = em + m;
-    }
+  const u64 em = before + block_scan<kT>(m, s.wave, all);
+  if (t < n && (by_mass ? (double)(base + em - m) < target && target <= (double)(base + em) : (u64)(t + 1) == want)) {
+    s.at[0] = s.sort[t];
+    s.at[1] = em;
   }
   __syncthreads();
   const Bound out = {s.at[0], s.at[1]};
@@ -269,100 +389,298 @@ __device__ Bound resolve(Shared& s, const T* row, int V, const Row& r, int b, in
   return out;
 }
 
-// One workgroup per row.
+// ---------------------------------------------------------------- slices of a row
+
+// The first composite of every slice, and the row's bins cleared.
 template <typename T>
+__global__ __launch_bounds__(kS) void sample_first_kernel(SampleArgs a) {
+  __shared__ u64 s_wave[kS / 64];
+  const int64_t r0 = blockIdx.y;
+  const T* row = static_cast<const T*>(a.logits) + r0 * a.ld;
+  RowSpace& sp = a.space[r0];
+  const int i0 = blockIdx.x * a.slice, i1 = min(i0 + a.slice, a.V), tid = threadIdx.x;
+  for (int b = blockIdx.x * kS + tid; b < kBins; b += a.slices * kS) {
+    sp.bin_count[b] = 0;
+    sp.bin_mass[b] = 0;
+  }
+  if (blockIdx.x == 0 && tid == 0) sp.n = 0;
+  u64 first = ~0ull;
+  for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int i) { first = min(first, composite(x, i)); });
+  first = block_min<kS>(first, s_wave);
+  if (tid == 0) sp.first[blockIdx.x] = first;
+}
+
+// A slice's share of the bins, or the weight that it keeps.
+template <typename T>
+__global__ __launch_bounds__(kS) void sample_bins_kernel(SampleArgs a) {
+  __shared__ u64 s_wave[kS / 64], s_mass[kBins];
+  __shared__ unsigned int s_count[kBins];
+  const int64_t r0 = blockIdx.y;
+  const T* row = static_cast<const T*>(a.logits) + r0 * a.ld;
+  RowSpace& sp = a.space[r0];
+  const int i0 = blockIdx.x * a.slice, i1 = min(i0 + a.slice, a.V), tid = threadIdx.x;
+  const Settings p = settings(a, r0);
+  const u64 first = block_min<kS>(tid < a.slices ? sp.first[tid] : ~0ull, s_wave);
+  if (first == ~0ull || p.first_only) return;
+  const Row r = row_of(first, p.temp);
+  if (!p.filtered) {
+    const double least = least_of(p.min_p);
+    u64 m = 0;
+    for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) {
+      if (exponent(r, x) >= least) m += weight(r, x);
+    });
+    m = block_reduce<kS>(m, s_wave, [](u64 x, u64 y) { return x + y; });
+    if (tid == 0) sp.mass[blockIdx.x] = m;
+    return;
+  }
+  for (int b = tid; b < kBins; b += kS) {
+    s_count[b] = 0;
+    s_mass[b] = 0;
+  }
+  __syncthreads();
+  for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) {
+    const int b = bin_of(r, x);
+    atomicAdd(&s_count[b], 1u);
+    atomicAdd(&s_mass[b], weight(r, x));
+  });
+  __syncthreads();
+  for (int b = tid; b < kBins; b += kS) {
+    if (!s_count[b]) continue;
+    atomicAdd(&sp.bin_count[b], s_count[b]);
+    atomicAdd(&sp.bin_mass[b], s_mass[b]);
+  }
+}
+
+// A slice's tokens that have to be sorted, and, where they are those of one bin, the weight that it keeps before it.
+// (The list's place is reserved once for the slice: 64 rows of 150000 took 25 us with an atomic per token.)
+template <typename T>
+__global__ __launch_bounds__(kS) void sample_gather_kernel(SampleArgs a) {
+  __shared__ u64 s_wave[kS / 64], s_at[8], s_list[kList];
+  __shared__ unsigned int s_n, s_to;
+  const int64_t r0 = blockIdx.y;
+  const T* row = static_cast<const T*>(a.logits) + r0 * a.ld;
+  RowSpace& sp = a.space[r0];
+  const int i0 = blockIdx.x * a.slice, i1 = min(i0 + a.slice, a.V), tid = threadIdx.x;
+  const Settings p = settings(a, r0);
+  if (p.first_only || !p.filtered) return;
+  const u64 first = block_min<kS>(tid < a.slices ? sp.first[tid] : ~0ull, s_wave);
+  if (first == ~0ull) return;
+  const Row r = row_of(first, p.temp);
+  const Ends e = find_ends<kS>(sp.bin_count, sp.bin_mass, p.top_k, p.top_p, s_wave, s_at);
+  const int what = gathered(e);
+  if (what == kGatherNone) return;
+  if (tid == 0) s_n = 0;
+  __syncthreads();
+  const double least = least_of(p.min_p);
+  u64 m = 0;
+  auto add = [&](float x, int i) {
+    const unsigned int at = atomicAdd(&s_n, 1u);
+    if (at < kList) s_list[at] = composite(x, i);
+  };
+  if (what == kGatherAll) {
+    for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int i) {
+      if (bin_of(r, x) <= e.last) add(x, i);
+    });
+  } else {
+    for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int i) {
+      const int b = bin_of(r, x);
+      if (b < e.last && exponent(r, x) >= least) m += weight(r, x);
+      if (b == e.last) add(x, i);
+    });
+    m = block_reduce<kS>(m, s_wave, [](u64 x, u64 y) { return x + y; });
+    if (tid == 0) sp.mass[blockIdx.x] = m;
+  }
+  __syncthreads();
+  const unsigned int n = s_n;
+  if (tid == 0 && n) s_to = atomicAdd(&sp.n, n);
+  __syncthreads();
+  for (unsigned int i = tid; i < n; i += kS)
+    if (s_to + i < kList) sp.list[s_to + i] = s_list[i];
+}
+
+// ---------------------------------------------------------------------- a row's token
+
+// SLICED: with what the kernels above have left; otherwise from the row alone.
+template <typename T, bool SLICED>
 __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
   __shared__ Shared s;
   const int64_t r0 = blockIdx.x;
   const T* row = static_cast<const T*>(a.logits) + r0 * a.ld;
   const int tid = threadIdx.x, V = a.V;
-  const float temp = a.temperature ? a.temperature[r0] : 1.0f;
-  const float top_p = a.top_p ? a.top_p[r0] : 1.0f, min_p = a.min_p ? a.min_p[r0] : 0.0f;
-  const int top_k = a.top_k ? a.top_k[r0] : 0;
-  // the largest
+  const Settings p = settings(a, r0);
+  RowSpace* sp = SLICED ? a.space + r0 : nullptr;
   u64 first = ~0ull;
-  for_range<T>(row, V, 0, V, tid, kT, [&](float x, int i) { first = min(first, composite(x, i)); });
-  first = block_reduce(first, s.wave, [](u64 p, u64 q) { return min(p, q); });
-  if (first == ~0ull || !(temp > 0.0f) || top_k == 1 || top_p <= 0.0f) {
+  if constexpr (SLICED) {
+    if (tid < a.slices) first = sp->first[tid];
+  } else {
+    for_range<T>(row, V, 0, V, tid, kT, [&](float x, int i) { first = min(first, composite(x, i)); });
+  }
+  first = block_min<kT>(first, s.wave);
+  if (first == ~0ull || p.first_only) {
     if (tid == 0) {
       a.token[r0] = first == ~0ull ? -1 : (int)(first & 0xfffffu);
       if (a.prob) a.prob[r0] = first == ~0ull ? 0.f : 1.f;
     }
     return;
   }
-  Row r;
-  r.top = logit_of(first);
-  r.scale = 1.4426950408889634 / (double)temp;
-  r.bins = fminf(64.0f / temp, 1e30f);
-  u64 bound = ~0ull;          // composites up to it are kept
-  if (top_k > 0 || top_p < 1.0f) {
-    for (int i = tid; i < kBins; i += kT) {
-      s.count[i] = 0;
-      s.mass[i] = 0;
-    }
-    __syncthreads();
-    for_range<T>(row, V, 0, V, tid, kT, [&](float x, int) {
-      const int b = bin_of(r, x);
-      atomicAdd(&s.count[b], 1u);
-      atomicAdd(&s.mass[b], weight(r, x));
-    });
-    __syncthreads();
-    // two bins a thread
-    const int t = 2 * tid;
-    u64 n_all, m_all;
-    const u64 c0 = s.count[t], c1 = s.count[t + 1], m0 = s.mass[t], m1 = s.mass[t + 1];
-    const u64 pc = block_scan(c0 + c1, s.wave, n_all) - c0 - c1;
-    const u64 pm = block_scan(m0 + m1, s.wave, m_all) - m0 - m1;
-    u64 sum = m_all;          // of what top-k keeps
-    int last_bin = kBins;     // the bin where top-k ends
-    if (top_k > 0 && (u64)top_k < n_all) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const u64 e = pc + (k ? c0 : 0), c = k ? c1 : c0;
-        if (e < (u64)top_k && (u64)top_k <= e + c) {
-          s.at[0] = t + k;
-          s.at[1] = top_k - e;
-          s.at[2] = pm + (k ? m0 : 0);
-          s.at[3] = c;
-        }
-      }
-      __syncthreads();
-      last_bin = (int)s.at[0];
-      const u64 want = s.at[1], base = s.at[2];
-      const int n = (int)s.at[3];
-      __syncthreads();
-      const Bound k = resolve(s, row, V, r, last_bin, n, false, want, base, 0.0, ~0ull);
-      bound = k.c;
-      sum = base + k.mass;
-    }
-    if (top_p < 1.0f) {
-      const double target = (double)top_p * (double)sum;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const u64 e = pm + (k ? m0 : 0), m = t + k == last_bin ? sum - e : k ? m1 : m0;
-        if (t + k <= last_bin && (double)e < target && target <= (double)(e + m)) {
-          s.at[0] = t + k;
-          s.at[2] = e;
-          s.at[3] = k ? c1 : c0;
-        }
-      }
-      __syncthreads();
-      const int b = (int)s.at[0], n = (int)s.at[3];
-      const u64 base = s.at[2];
-      __syncthreads();
-      bound = min(bound, resolve(s, row, V, r, b, n, true, 0, base, target, bound).c);
-    }
-  }
-  const double least = min_p > 0.0f ? fmin(log2((double)min_p), 0.0) : -INFINITY;
-  auto kept = [&](float x, int i) { return composite(x, i) <= bound && exponent(r, x) >= least; };
-  // the segment of the row in which the distribution passes u, cut in 16 by the waves' sums until a lane has one token
+  const Row r = row_of(first, p.temp);
+  const double least = least_of(p.min_p);
   float u = a.u[r0];
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
+  u64 bound = ~0ull;          // composites up to it are kept
+  int what = kGatherNone;
+  int n = 0;                  // composites in s.list
+  if (p.filtered) {
+    for (int i = tid; i < kBins; i += kT) {
+      s.count[i] = SLICED ? sp->bin_count[i] : 0;
+      s.mass[i] = SLICED ? sp->bin_mass[i] : 0;
+    }
+    __syncthreads();
+    if constexpr (!SLICED) {
+      for_range<T>(row, V, 0, V, tid, kT, [&](float x, int) {
+        const int b = bin_of(r, x);
+        atomicAdd(&s.count[b], 1u);
+        atomicAdd(&s.mass[b], weight(r, x));
+      });
+      __syncthreads();
+    }
+    const Ends e = find_ends<kT>(s.count, s.mass, p.top_k, p.top_p, s.wave, s.at);
+    what = gathered(e);
+    if constexpr (SLICED) {
+      if (what != kGatherNone) n = (int)(what == kGatherAll ? e.count : e.in_bin);
+      for (int i = tid; i < n; i += kT) s.list[i] = sp->list[i];
+    } else if (what == kGatherAll) {
+      n = (int)e.count;
+      if (tid == 0) s.n = 0;
+      __syncthreads();
+      for_range<T>(row, V, 0, V, tid, kT, [&](float x, int i) {
+        if (bin_of(r, x) > e.last) return;
+        const unsigned int at = atomicAdd(&s.n, 1u);
+        if (at < kList) s.list[at] = composite(x, i);
+      });
+    } else {
+      what = kGatherNone;
+    }
+    __syncthreads();
+    const bool listed = what != kGatherNone;
+    auto each = [&](auto&& f) __attribute__((always_inline)) {
+      if (listed) {
+        for (int i = tid; i < n; i += kT) f(logit_of(s.list[i]), s.list[i]);
+      } else {
+        for_range<T>(row, V, 0, V, tid, kT, [&](float x, int i) { f(x, composite(x, i)); });
+      }
+    };
+    u64 sum = e.m_all;          // the weight that top-k keeps
+    if (e.by_k) {
+      const Bound k = resolve(s, each, r, e.last, (int)e.in_bin, false, e.want, e.base, 0.0, ~0ull);
+      bound = k.c;
+      sum = e.base + k.mass;
+    }
+    if (p.top_p < 1.0f) {
+      const double target = (double)p.top_p * (double)sum;
+      const int t = 2 * tid;
+      const u64 m0 = s.mass[t], m1 = s.mass[t + 1];
+      u64 total;
+      const u64 pm = block_scan<kT>(m0 + m1, s.wave, total) - m0 - m1;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const u64 ahead = pm + (k ? m0 : 0), m = e.by_k && t + k == e.last ? sum - ahead : k ? m1 : m0;
+        if ((!e.by_k || t + k <= e.last) && (double)ahead < target && target <= (double)(ahead + m)) {
+          s.at[0] = t + k;
+          s.at[2] = ahead;
+          s.at[3] = s.count[t + k];
+        }
+      }
+      __syncthreads();
+      const int b = (int)s.at[0], in_bin = (int)s.at[3];
+      const u64 base = s.at[2];
+      __syncthreads();
+      bound = min(bound, resolve(s, each, r, b, in_bin, true, 0, base, target, bound).c);
+    }
+  }
+  auto kept = [&](float x, int i) { return composite(x, i) <= bound && exponent(r, x) >= least; };
+  if (what == kGatherAll) {
+    // all that is kept is in the list: its weight by 1024 parts of the vocabulary, then within the part where u falls
+    u64 m[kList / kT], all = 0;
+#pragma unroll
+    for (int k = 0; k < kList / kT; ++k) {
+      const int i = tid + k * kT;
+      const u64 c = i < n ? s.list[i] : ~0ull;
+      const float x = logit_of(c);
+      m[k] = i < n && c <= bound && exponent(r, x) >= least ? weight(r, x) : 0;
+      all += m[k];
+    }
+    all = block_reduce<kT>(all, s.wave, [](u64 x, u64 y) { return x + y; });
+    const double target = (double)u * (double)all;
+    u64 base = 0;
+    int part = -1;
+#pragma unroll
+    for (int level = 0; level < 2; ++level) {
+      s.mass[tid] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kList / kT; ++k) {
+        if (!m[k]) continue;
+        const int i = (int)(s.list[tid + k * kT] & 0xfffffu);
+        if (level == 0) atomicAdd(&s.mass[i >> 10], m[k]);
+        else if (i >> 10 == part) s.mass[i & 1023] = m[k];
+      }
+      __syncthreads();
+      const u64 mine = s.mass[tid];
+      u64 total;
+      const u64 upto = base + block_scan<kT>(mine, s.wave, total);
+      if ((double)upto > target && !((double)(upto - mine) > target)) {
+        if (level == 0) {
+          s.at[0] = tid;
+          s.at[1] = upto - mine;
+        } else {
+          a.token[r0] = (part << 10) + tid;
+          if (a.prob) a.prob[r0] = (float)((double)mine / (double)all);
+        }
+      }
+      __syncthreads();
+      if (level == 0) {
+        part = (int)s.at[0];
+        base = s.at[1];
+      }
+    }
+    return;
+  }
+  // the weight that every slice keeps, where it is known
+  const bool by_slice = SLICED && (!p.filtered || what == kGatherBin);
+  if (by_slice) {
+    __syncthreads();
+    if (tid < kMaxSlices) s.mass[tid] = tid < a.slices ? sp->mass[tid] : 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kT) {
+      const u64 c = s.list[i];
+      const float x = logit_of(c);
+      if (c <= bound && exponent(r, x) >= least) atomicAdd(&s.mass[(int)(c & 0xfffffu) / a.slice], weight(r, x));
+    }
+    __syncthreads();
+  }
+  // the segment of the row in which the distribution passes u, cut in 16 by the waves' sums until a lane has one token
   int i0 = 0, i1 = V;
   u64 base = 0;
   double all = 0.0, target = 0.0;
+  bool whole = true;
+  if (by_slice) {
+    u64 sum;
+    const u64 mine = tid < kMaxSlices ? s.mass[tid] : 0, upto = block_scan<kT>(mine, s.wave, sum);
+    all = (double)sum;
+    target = (double)u * all;
+    if ((double)upto > target && !((double)(upto - mine) > target)) {
+      s.at[0] = tid;
+      s.at[1] = upto - mine;
+    }
+    __syncthreads();
+    i0 = (int)s.at[0] * a.slice;
+    i1 = min(i0 + a.slice, V);
+    base = s.at[1];
+    whole = false;
+  }
   const int wave = tid >> 6, lane = tid & 63;
-  for (bool whole = true; whole || i1 - i0 > kT; whole = false) {
+  for (; whole || i1 - i0 > kT; whole = false) {
     const int seg = (i1 - i0 + 15) / 16, a0 = min(i0 + wave * seg, i1), a1 = min(a0 + seg, i1);
     u64 m = 0;
     for_range<T>(row, V, a0, a1, lane, 64, [&](float x, int i) {
@@ -392,11 +710,49 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
     if (x > -INFINITY && kept(x, i)) m = weight(r, x);
   }
   u64 sum;
-  const u64 upto = base + block_scan(m, s.wave, sum);
+  const u64 upto = base + block_scan<kT>(m, s.wave, sum);
   if ((double)upto > target && !((double)(upto - m) > target)) {
     a.token[r0] = i;
     if (a.prob) a.prob[r0] = (float)((double)m / all);
   }
+}
+
+// Slices of a row: a 16-byte piece or more for every thread, so many that the chip has some 1024 workgroups.
+constexpr int kAlone = 8192;
+struct Slices {
+  int n, tokens;
+};
+Slices slices_of(int64_t rows, int64_t V, size_t elem) {
+  const int64_t unit = kS * (16 / (int64_t)elem);
+  int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(rows, 1));
+  want = std::min<int64_t>(std::min<int64_t>(want, (V + unit - 1) / unit), kMaxSlices);
+  const int64_t tokens = ((V + want - 1) / want + unit - 1) / unit * unit;
+  return {(int)((V + tokens - 1) / tokens), (int)tokens};
+}
+
+template <typename T>
+catq_status launch_sample(SampleArgs a, int64_t rows, hipStream_t stream) {
+  const double bytes = (double)rows * a.V * sizeof(T);
+  if (a.V <= kAlone) {
+    CATQ_TRACED(stream, "sample_kernel<alone>", 0.0, bytes, rows, a.V, 1,
+                hipLaunchKernelGGL((sample_kernel<T, false>), dim3((unsigned)rows), dim3(kT), 0, stream, a));
+    CATQ_CHECK_LAUNCH("sample");
+    return CATQ_OK;
+  }
+  const Slices sl = slices_of(rows, a.V, sizeof(T));
+  a.slices = sl.n;
+  a.slice = sl.tokens;
+  const dim3 grid((unsigned)sl.n, (unsigned)rows);
+  CATQ_TRACED(stream, "sample_first_kernel", 0.0, bytes, rows, a.V, sl.n,
+              hipLaunchKernelGGL((sample_first_kernel<T>), grid, dim3(kS), 0, stream, a));
+  CATQ_TRACED(stream, "sample_bins_kernel", 0.0, bytes, rows, a.V, sl.n,
+              hipLaunchKernelGGL((sample_bins_kernel<T>), grid, dim3(kS), 0, stream, a));
+  CATQ_TRACED(stream, "sample_gather_kernel", 0.0, bytes, rows, a.V, sl.n,
+              hipLaunchKernelGGL((sample_gather_kernel<T>), grid, dim3(kS), 0, stream, a));
+  CATQ_TRACED(stream, "sample_kernel", 0.0, 0.0, rows, a.V, 1,
+              hipLaunchKernelGGL((sample_kernel<T, true>), dim3((unsigned)rows), dim3(kT), 0, stream, a));
+  CATQ_CHECK_LAUNCH("sample");
+  return CATQ_OK;
 }
 
 }  // namespace
@@ -405,8 +761,8 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
 using namespace catq;
 
 extern "C" size_t catq_aux_sample_workspace_bytes(int64_t rows, int64_t V) {
-  if (rows <= 0 || V <= 0) return 0;
-  return 0;
+  if (rows <= 0 || rows > 65535 || V <= kAlone || V > (1 << 20)) return 0;
+  return (size_t)rows * sizeof(RowSpace);
 }
 
 extern "C" catq_status catq_aux_sample(const void* logits, catq_dtype dtype, int64_t rows, int64_t V, int64_t ld,
@@ -419,9 +775,8 @@ extern "C" catq_status catq_aux_sample(const void* logits, catq_dtype dtype, int
   CATQ_REQUIRE(logits && u && token, CATQ_ERR_NULL, "logits, u and token must not be NULL");
   CATQ_REQUIRE(dtype_ok(dtype), CATQ_ERR_DTYPE, "logits must be fp32 or bf16");
   CATQ_REQUIRE(V > 0 && V <= (1 << 20), CATQ_ERR_SHAPE, "V must be 1 .. 2^20");
-  // (a launch has fewer than 2^32 threads along x)
-  CATQ_REQUIRE(rows < (1 << 22) && ld >= V && count_ok(rows, ld), CATQ_ERR_SHAPE,
-               "ld must be >= V, rows below 2^22 and rows * ld within 2^38");
+  CATQ_REQUIRE(rows <= 65535 && ld >= V && count_ok(rows, ld), CATQ_ERR_SHAPE,
+               "ld must be >= V, rows at most 65535 and rows * ld within 2^38");
   auto at4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; };
   CATQ_REQUIRE(aligned16(logits) && at4(temperature) && at4(top_k) && at4(top_p) && at4(min_p) && at4(u) &&
                    at4(token) && at4(prob) && aligned16(workspace),
@@ -429,11 +784,7 @@ extern "C" catq_status catq_aux_sample(const void* logits, catq_dtype dtype, int
   const size_t need = catq_aux_sample_workspace_bytes(rows, V);
   CATQ_REQUIRE(need == 0 || (workspace && workspace_bytes >= need), CATQ_ERR_WORKSPACE,
                "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
-  const SampleArgs a{logits, ld, (int32_t)V, temperature, top_k, top_p, min_p, u, token, prob};
-  const double bytes = (double)rows * (double)V * (double)dtype_size(dtype);
-  auto kernel = dtype == CATQ_F32 ? sample_kernel<float> : sample_kernel<bf16>;
-  CATQ_TRACED(stream, "sample_kernel", 0.0, bytes, rows, V, 1,
-              hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kT), 0, stream, a));
-  CATQ_CHECK_LAUNCH("sample");
-  return CATQ_OK;
+  const SampleArgs a{logits, ld, (int32_t)V, temperature, top_k, top_p, min_p, u, token, prob,
+                     static_cast<RowSpace*>(workspace), 1, (int32_t)V};
+  return dtype == CATQ_F32 ? launch_sample<float>(a, rows, stream) : launch_sample<bf16>(a, rows, stream);
 }

@@ -15,33 +15,36 @@ pytestmark = pytest.mark.gpu
 DELTA = 2.0 ** -21
 
 
-def _one(x, T, k, p, m, u, dp=0.0, du=0.0):
-    """(token, prob) of one row of float64 logits; dp, du move the borders of top-p and u."""
+def _all(x, T, k, p, m, u):
+    """The (token, prob) that one row of float64 logits can give, with the borders of top-p and u moved by DELTA."""
     ok = x > -math.inf                                   # (False for NaN)
     if not ok.any():
-        return -1, 0.0
+        return {(-1, 0.0)}
     ids = np.flatnonzero(ok)
     order = ids[np.argsort(-x[ids], kind="stable")]
     if not T > 0:
-        return int(order[0]), 1.0
+        return {(int(order[0]), 1.0)}
     top = x[order[0]]
     with np.errstate(invalid="ignore"):
         w = np.where(x[order] == top, 1.0, np.exp((x[order] - top) / T))
     if k > 0:
         order, w = order[:k], w[:k]
-    if p < 1:
-        before = np.concatenate([[0.0], np.cumsum(w)[:-1]])
-        n = max(1, int((before < (p + dp) * w.sum()).sum()))
-        order, w = order[:n], w[:n]
-    if m > 0:
-        n = max(1, int((w >= m).sum()))
-        order, w = order[:n], w[:n]
-    by_id = np.argsort(order)
-    order, w = order[by_id], w[by_id]
-    cum = np.cumsum(w)
     u = 0.0 if not u > 0 else min(u, 1 - 2.0 ** -24)
-    at = min(int((cum <= (u + du) * cum[-1]).sum()), len(order) - 1)
-    return int(order[at]), float(w[at] / cum[-1])
+    sizes = {len(order)}
+    if p < 1:
+        before, whole = np.concatenate([[0.0], np.cumsum(w)[:-1]]), w.sum()
+        sizes = {max(1, int((before < (p + dp) * whole).sum())) for dp in (0.0, -DELTA, DELTA)}
+    if m > 0:
+        sizes = {min(n, max(1, int((w >= m).sum()))) for n in sizes}
+    out = set()
+    for n in sizes:
+        by_id = np.argsort(order[:n])
+        ids, wi = order[:n][by_id], w[:n][by_id]
+        cum = np.cumsum(wi)
+        for du in (0.0, -DELTA, DELTA):
+            at = min(int((cum <= (u + du) * cum[-1]).sum()), n - 1)
+            out.add((int(ids[at]), float(wi[at] / cum[-1])))
+    return out
 
 
 def _check(catq, logits, u, T=None, k=None, p=None, m=None, ld=None, repeat=True):
@@ -64,8 +67,7 @@ def _check(catq, logits, u, T=None, k=None, p=None, m=None, ld=None, repeat=True
     for r in range(n):
         row = [np.float32(v[r]).astype(float) if v is not None else d for v, d in ((T, 1.0), (p, 1.0), (m, 0.0))]
         kk = 0 if k is None else k[r]
-        want = {_one(x[r], row[0], kk, row[1], row[2], u32[r], dp, du) for dp in (0.0, -DELTA, DELTA)
-                for du in (0.0, -DELTA, DELTA)}
+        want = _all(x[r], row[0], kk, row[1], row[2], u32[r])
         got = int(token[r]), float(prob[r])
         near = [q for t, q in want if t == got[0]]
         assert near, (r, got, want, [None if v is None else v[r] for v in (T, k, p, m)], u[r])
@@ -83,7 +85,7 @@ def _gen(seed):
     return g
 
 
-SIZES = [(1, 1, None), (3, 2, None), (5, 7, 9), (4, 100, None), (6, 1000, 1003), (3, 4097, None), (8, 32000, None),
+SIZES = [(1, 1, None), (3, 2, None), (5, 7, 9), (4, 100, None), (6, 1000, 1003), (3, 4097, None), (3, 8192, 8195), (3, 8193, None), (8, 32000, None),
          (5, 50257, 50261), (4, 150000, None), (1, 262147, None), (70, 300, 301), (2, 1 << 20, None)]
 
 
