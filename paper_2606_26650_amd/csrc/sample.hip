@@ -13,7 +13,7 @@
 // Steps.  A row's tokens go into 2048 bins of 1/64 of exp's argument below the largest logit, with their number and
 // their weight.  The bins tell where top-k (or, without it, top-p) ends.  Where the tokens up to that bin are few, they
 // are gathered and the rest happens in LDS; where they are many, that bin's tokens are, and the weight before it is summed
-// by slices of the row, of which the one where u falls is read again.  Only the bins in which a filter ends are sorted.
+// by slices of the row, of which the one where u falls is read again.  Only in the bins in which a filter ends are tokens compared.
 // Without top-k and top-p no bins are needed, only the weight of every slice.
 //
 // Rows of more than kAlone tokens are read by several workgroups each: the largest logit of every slice, then bins
@@ -28,13 +28,12 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kT = 1024;              // threads of the workgroup that picks a row's token
+constexpr int kT = 256;               // threads of the workgroup that picks a row's token
 constexpr int kS = 256;               // threads of one that reads a slice
 constexpr int kBins = 2048;
 constexpr int kList = 4096;           // composites that are gathered
-constexpr int kSort = 1024;           // that are sorted
 constexpr int kOne = 43;              // a weight of 1 is 2^43
-constexpr int kMaxSlices = 256;
+constexpr int kMaxSlices = 256;       // (kT)
 
 // What the workgroups of a row leave for those after them
 struct RowSpace {
@@ -172,17 +171,29 @@ __device__ __forceinline__ void for_range(const T* row, int V, int i0, int i1, i
   }
 }
 
-__device__ __forceinline__ u64 shfl_up64(u64 v, int d) { return __shfl_up(v, d, 64); }
+// v plus what another lane of the wave has, by a data-parallel move (0 where there is none)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 add_moved(u64 v) {
+  const unsigned int lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)v, CTRL, ROWS, 0xf, false);
+  const unsigned int hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(v >> 32), CTRL, ROWS, 0xf, false);
+  return v + (((u64)hi << 32) | lo);
+}
+// Inclusive prefix sum over a wave: within rows of 16 lanes by shifts of 1, 2, 4 and 8, then a row's last lane to the
+// next row, and lane 31 to the upper half.  (Six shuffles through LDS took 600 cycles.)
+__device__ __forceinline__ u64 wave_scan(u64 v) {
+  v = add_moved<0x111, 0xf>(v);
+  v = add_moved<0x112, 0xf>(v);
+  v = add_moved<0x114, 0xf>(v);
+  v = add_moved<0x118, 0xf>(v);
+  v = add_moved<0x142, 0xa>(v);
+  return add_moved<0x143, 0xc>(v);
+}
 
 // Inclusive prefix sum over the workgroup; `total` is the whole.  s: one value per wave.
 template <int NT>
 __device__ __forceinline__ u64 block_scan(u64 v, u64* s, u64& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const u64 o = shfl_up64(v, d);
-    if (lane >= d) v += o;
-  }
+  v = wave_scan(v);
   __syncthreads();
   if (lane == 63) s[wave] = v;
   __syncthreads();
@@ -207,6 +218,12 @@ __device__ __forceinline__ u64 block_reduce(u64 v, u64* s, F&& f) {
 #pragma unroll
   for (int w = 1; w < NT / 64; ++w) v = f(v, s[w]);
   return v;
+}
+template <int NT>
+__device__ __forceinline__ u64 block_sum(u64 v, u64* s) {
+  u64 total;
+  block_scan<NT>(v, s, total);
+  return total;
 }
 template <int NT>
 __device__ __forceinline__ u64 block_min(u64 v, u64* s) {
@@ -275,10 +292,11 @@ __device__ __forceinline__ Ends find_ends(const unsigned int* count, const u64* 
 }
 
 struct Shared {
-  u64 list[kList];      // what has been gathered
-  u64 sort[kSort];      // of one bin, in order
-  u64 mass[kBins];      // the row's bins
-  u64 part_mass[kBins];
+  u64 list[kList];        // what has been gathered
+  u64 few[kT];            // the last tokens in question
+  u64 weight[kT];         // and what they weigh
+  u64 mass[kBins];        // the row's bins
+  u64 part_mass[kBins];   // parts of one of them
   unsigned int count[kBins];
   unsigned int part_count[kBins];
   u64 wave[kT / 64];
@@ -286,102 +304,128 @@ struct Shared {
   unsigned int n;
 };
 
-// s.sort[0 .. n) in ascending order (n <= kSort)
-__device__ __forceinline__ void sort_list(Shared& s, int n) {
-  int size = 2;
-  while (size < n) size <<= 1;
-  if (n + (int)threadIdx.x < size) s.sort[n + threadIdx.x] = ~0ull;
-  __syncthreads();
-  for (int k = 2; k <= size; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      const int p = threadIdx.x;
-      if (p < size / 2) {
-        const int a = 2 * (p & ~(j - 1)) + (p & (j - 1)), b = a + j;
-        const u64 x = s.sort[a], y = s.sort[b];
-        if ((x > y) == ((a & k) == 0)) {
-          s.sort[a] = y;
-          s.sort[b] = x;
-        }
-      }
-      __syncthreads();
+// Of N sums in LDS, the one where base + their running sum passes `target` (in s.at: its index, what is before it,
+// itself).
+template <int N>
+__device__ __forceinline__ void find_passing(Shared& s, const u64* sums, u64 base, double target) {
+  constexpr int B = N / kT;
+  const int t = B * threadIdx.x;
+  u64 m[B], ms = 0, all;
+#pragma unroll
+  for (int i = 0; i < B; ++i) {
+    m[i] = sums[t + i];
+    ms += m[i];
+  }
+  u64 em = base + block_scan<kT>(ms, s.wave, all) - ms;
+#pragma unroll
+  for (int i = 0; i < B; ++i) {
+    if (!((double)em > target) && (double)(em + m[i]) > target) {
+      s.at[0] = t + i;
+      s.at[1] = em;
+      s.at[2] = m[i];
     }
+    em += m[i];
+  }
+  __syncthreads();
 }
 
-// Of the tokens in bin b (n of them): the composite of the last one that is kept, and their mass up to it.
-// By count: the first `want` of them are kept.  By mass: those before which the mass (with `base`) is below `target`,
-// of the ones with c <= most.  each(f) calls f(logit, composite) for every token of the row that may be in the bin.
-struct Bound {
-  u64 c, mass;
+// A filter's end in a bin of n tokens.  By count: the first `want` of them are kept.  By mass: those before which
+// the mass (`base` before the bin) is below `target`.
+struct Cut {
+  int bin, n;
+  bool by_mass;
+  u64 want, base;
+  double target;
 };
+struct Bound {
+  u64 c, mass;      // the composite of the last token that is kept, the weight of the bin's up to it
+};
+
+// each(f) calls f(logit, composite) for all tokens of the row that may be in the bin; those with c <= most count.
+// Where more than one per thread are left, the interval of composites in question is cut to one of up to 2048 parts, again
+// and again; then each thread counts the tokens ahead of its own and their weight.  (Sorting them took three times
+// as long for 100 tokens, and more for more.)
 template <typename Each>
-__device__ __forceinline__ Bound resolve(Shared& s, Each&& each, const Row& r, int b, int n, bool by_mass, u64 want,
-                                         u64 base, double target, u64 most) {
-  u64 lo = 0, hi = most, before = 0;      // composites lo .. hi are in question; the mass of those below lo
-  // more than are sorted: the interval is cut to one of up to 2048 parts, again and again
-  while (n > kSort) {
+__device__ __forceinline__ Bound cut_bin(Shared& s, Each&& each, const Row& r, Cut q, u64 most) {
+  u64 lo = 0, hi = most, before = 0;      // composites lo .. hi are in question; the weight of the bin's below lo
+  const int t = threadIdx.x;
+#pragma unroll 1
+  while (q.n > kT) {
     u64 least = ~0ull, last = 0;
     each([&](float x, u64 c) {
-      if (bin_of(r, x) != b || c < lo || c > hi) return;
+      if (bin_of(r, x) != q.bin || c < lo || c > hi) return;
       least = min(least, c);
       last = max(last, c);
     });
     lo = block_min<kT>(least, s.wave);
-    hi = block_reduce<kT>(last, s.wave, [](u64 p, u64 q) { return max(p, q); });
+    hi = ~block_min<kT>(~last, s.wave);
     const int bits = 64 - __builtin_clzll((hi - lo) | 1);
     const int shift = bits > 11 ? bits - 11 : 0;
-    for (int i = threadIdx.x; i < kBins; i += kT) {
+    for (int i = t; i < kBins; i += kT) {
       s.part_count[i] = 0;
       s.part_mass[i] = 0;
     }
     __syncthreads();
     each([&](float x, u64 c) {
-      if (bin_of(r, x) != b || c < lo || c > hi) return;
+      if (bin_of(r, x) != q.bin || c < lo || c > hi) return;
       atomicAdd(&s.part_count[(c - lo) >> shift], 1u);
       atomicAdd(&s.part_mass[(c - lo) >> shift], weight(r, x));
     });
     __syncthreads();
-    const int t = 2 * threadIdx.x;
-    u64 all;
-    const u64 c0 = s.part_count[t], c1 = s.part_count[t + 1], m0 = s.part_mass[t], m1 = s.part_mass[t + 1];
-    const u64 pc = block_scan<kT>(c0 + c1, s.wave, all) - c0 - c1, pm = block_scan<kT>(m0 + m1, s.wave, all) - m0 - m1;
+    constexpr int B = kBins / kT;
+    u64 cs = 0, ms = 0, all;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const u64 ec = pc + (k ? c0 : 0), em = pm + (k ? m0 : 0), c = k ? c1 : c0, m = k ? m1 : m0;
-      const bool here = by_mass ? (double)(base + before + em) < target && target <= (double)(base + before + em + m)
-                                : ec < want && want <= ec + c;
+    for (int k = 0; k < B; ++k) {
+      cs += s.part_count[B * t + k];
+      ms += s.part_mass[B * t + k];
+    }
+    u64 ec = block_scan<kT>(cs, s.wave, all) - cs, em = q.base + before + block_scan<kT>(ms, s.wave, all) - ms;
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      const u64 c = s.part_count[B * t + k], m = s.part_mass[B * t + k];
+      const bool here = q.by_mass ? (double)em < q.target && q.target <= (double)(em + m)
+                                  : ec < q.want && q.want <= ec + c;
       if (here) {
-        s.at[0] = t + k;
+        s.at[0] = B * t + k;
         s.at[1] = ec;
-        s.at[2] = em;
+        s.at[2] = em - q.base;
         s.at[3] = c;
       }
+      ec += c;
+      em += m;
     }
     __syncthreads();
-    const u64 part = s.at[0];
-    before += s.at[2];
-    want -= by_mass ? 0 : s.at[1];
-    n = (int)s.at[3];
-    lo += part << shift;
+    before = s.at[2];
+    q.want -= q.by_mass ? 0 : s.at[1];
+    q.n = (int)s.at[3];
+    lo += s.at[0] << shift;
     hi = min(hi, lo + ((1ull << shift) - 1));
     __syncthreads();
   }
-  if (threadIdx.x == 0) s.n = 0;
+  if (t == 0) s.n = 0;
   __syncthreads();
   each([&](float x, u64 c) {
-    if (bin_of(r, x) != b || c < lo || c > hi) return;
+    if (bin_of(r, x) != q.bin || c < lo || c > hi) return;
     const unsigned int at = atomicAdd(&s.n, 1u);
-    if (at < kSort) s.sort[at] = c;
+    if (at < kT) s.few[at] = c;
   });
   __syncthreads();
-  n = (int)min(s.n, (unsigned)kSort);
-  sort_list(s, n);
-  const int t = threadIdx.x;
-  const u64 m = t < n ? weight(r, logit_of(s.sort[t])) : 0;
-  u64 all;
-  const u64 em = before + block_scan<kT>(m, s.wave, all);
-  if (t < n && (by_mass ? (double)(base + em - m) < target && target <= (double)(base + em) : (u64)(t + 1) == want)) {
-    s.at[0] = s.sort[t];
-    s.at[1] = em;
+  const int n = (int)min(s.n, (unsigned)kT);
+  const u64 c = t < n ? s.few[t] : 0, m = t < n ? weight(r, logit_of(c)) : 0;
+  s.weight[t] = m;
+  __syncthreads();
+  u64 em = before, rank = 0;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const bool ahead = s.few[i] < c;
+    rank += ahead ? 1 : 0;
+    em += ahead ? s.weight[i] : 0;
+  }
+  const bool here = q.by_mass ? (double)(q.base + em) < q.target && q.target <= (double)(q.base + em + m)
+                              : rank + 1 == q.want;
+  if (t < n && here) {
+    s.at[0] = c;
+    s.at[1] = em + m;
   }
   __syncthreads();
   const Bound out = {s.at[0], s.at[1]};
@@ -429,7 +473,7 @@ __global__ __launch_bounds__(kS) void sample_bins_kernel(SampleArgs a) {
     for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) {
       if (exponent(r, x) >= least) m += weight(r, x);
     });
-    m = block_reduce<kS>(m, s_wave, [](u64 x, u64 y) { return x + y; });
+    m = block_sum<kS>(m, s_wave);
     if (tid == 0) sp.mass[blockIdx.x] = m;
     return;
   }
@@ -487,7 +531,7 @@ __global__ __launch_bounds__(kS) void sample_gather_kernel(SampleArgs a) {
       if (b < e.last && exponent(r, x) >= least) m += weight(r, x);
       if (b == e.last) add(x, i);
     });
-    m = block_reduce<kS>(m, s_wave, [](u64 x, u64 y) { return x + y; });
+    m = block_sum<kS>(m, s_wave);
     if (tid == 0) sp.mass[blockIdx.x] = m;
   }
   __syncthreads();
@@ -562,40 +606,44 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
       what = kGatherNone;
     }
     __syncthreads();
-    const bool listed = what != kGatherNone;
-    auto each = [&](auto&& f) __attribute__((always_inline)) {
-      if (listed) {
-        for (int i = tid; i < n; i += kT) f(logit_of(s.list[i]), s.list[i]);
-      } else {
-        for_range<T>(row, V, 0, V, tid, kT, [&](float x, int i) { f(x, composite(x, i)); });
-      }
-    };
     u64 sum = e.m_all;          // the weight that top-k keeps
-    if (e.by_k) {
-      const Bound k = resolve(s, each, r, e.last, (int)e.in_bin, false, e.want, e.base, 0.0, ~0ull);
-      bound = k.c;
-      sum = e.base + k.mass;
-    }
-    if (p.top_p < 1.0f) {
-      const double target = (double)p.top_p * (double)sum;
-      const int t = 2 * tid;
-      const u64 m0 = s.mass[t], m1 = s.mass[t + 1];
-      u64 total;
-      const u64 pm = block_scan<kT>(m0 + m1, s.wave, total) - m0 - m1;
+    Cut q = {e.last, (int)e.in_bin, false, e.want, e.base, 0.0};
+#pragma unroll 1
+    for (int filter = e.by_k ? 0 : 1; filter < (p.top_p < 1.0f ? 2 : 1); ++filter) {
+      if (filter == 1) {
+        q.by_mass = true;
+        q.target = (double)p.top_p * (double)sum;
+        constexpr int B = kBins / kT;
+        const int t = B * tid;
+        u64 ms = 0, total;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const u64 ahead = pm + (k ? m0 : 0), m = e.by_k && t + k == e.last ? sum - ahead : k ? m1 : m0;
-        if ((!e.by_k || t + k <= e.last) && (double)ahead < target && target <= (double)(ahead + m)) {
-          s.at[0] = t + k;
-          s.at[2] = ahead;
-          s.at[3] = s.count[t + k];
+        for (int k = 0; k < B; ++k) ms += s.mass[t + k];
+        u64 ahead = block_scan<kT>(ms, s.wave, total) - ms;
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+          const u64 m = e.by_k && t + k == e.last ? sum - ahead : s.mass[t + k];
+          if ((!e.by_k || t + k <= e.last) && (double)ahead < q.target && q.target <= (double)(ahead + m)) {
+            s.at[0] = t + k;
+            s.at[2] = ahead;
+            s.at[3] = s.count[t + k];
+          }
+          ahead += m;
         }
+        __syncthreads();
+        q.bin = (int)s.at[0];
+        q.base = s.at[2];
+        q.n = (int)s.at[3];
+        __syncthreads();
       }
-      __syncthreads();
-      const int b = (int)s.at[0], in_bin = (int)s.at[3];
-      const u64 base = s.at[2];
-      __syncthreads();
-      bound = min(bound, resolve(s, each, r, b, in_bin, true, 0, base, target, bound).c);
+      const Bound end = cut_bin(s, [&](auto&& f) __attribute__((always_inline)) {
+        if (what != kGatherNone) {
+          for (int i = tid; i < n; i += kT) f(logit_of(s.list[i]), s.list[i]);
+        } else {
+          for_range<T>(row, V, 0, V, tid, kT, [&](float x, int i) { f(x, composite(x, i)); });
+        }
+      }, r, q, bound);
+      bound = min(bound, end.c);
+      sum = q.base + end.mass;
     }
   }
   auto kept = [&](float x, int i) { return composite(x, i) <= bound && exponent(r, x) >= least; };
@@ -610,13 +658,13 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
       m[k] = i < n && c <= bound && exponent(r, x) >= least ? weight(r, x) : 0;
       all += m[k];
     }
-    all = block_reduce<kT>(all, s.wave, [](u64 x, u64 y) { return x + y; });
+    all = block_sum<kT>(all, s.wave);
     const double target = (double)u * (double)all;
     u64 base = 0;
     int part = -1;
-#pragma unroll
+#pragma unroll 1
     for (int level = 0; level < 2; ++level) {
-      s.mass[tid] = 0;
+      for (int i = tid; i < 1024; i += kT) s.mass[i] = 0;
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < kList / kT; ++k) {
@@ -626,23 +674,15 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
         else if (i >> 10 == part) s.mass[i & 1023] = m[k];
       }
       __syncthreads();
-      const u64 mine = s.mass[tid];
-      u64 total;
-      const u64 upto = base + block_scan<kT>(mine, s.wave, total);
-      if ((double)upto > target && !((double)(upto - mine) > target)) {
-        if (level == 0) {
-          s.at[0] = tid;
-          s.at[1] = upto - mine;
-        } else {
-          a.token[r0] = (part << 10) + tid;
-          if (a.prob) a.prob[r0] = (float)((double)mine / (double)all);
-        }
-      }
-      __syncthreads();
+      find_passing<1024>(s, s.mass, base, target);
       if (level == 0) {
         part = (int)s.at[0];
         base = s.at[1];
       }
+    }
+    if (tid == 0) {
+      a.token[r0] = (part << 10) + (int)s.at[0];
+      if (a.prob) a.prob[r0] = (float)((double)s.at[2] / (double)all);
     }
     return;
   }
@@ -659,61 +699,44 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
     }
     __syncthreads();
   }
-  // the segment of the row in which the distribution passes u, cut in 16 by the waves' sums until a lane has one token
+  // the part of the row in which the distribution passes u: a thread sums consecutive tokens, and the part becomes those
+  // of the thread where it passes, until that is one
   int i0 = 0, i1 = V;
   u64 base = 0;
   double all = 0.0, target = 0.0;
   bool whole = true;
   if (by_slice) {
-    u64 sum;
-    const u64 mine = tid < kMaxSlices ? s.mass[tid] : 0, upto = block_scan<kT>(mine, s.wave, sum);
-    all = (double)sum;
+    all = (double)block_sum<kT>(tid < kMaxSlices ? s.mass[tid] : 0, s.wave);
     target = (double)u * all;
-    if ((double)upto > target && !((double)(upto - mine) > target)) {
-      s.at[0] = tid;
-      s.at[1] = upto - mine;
-    }
-    __syncthreads();
+    find_passing<kMaxSlices>(s, s.mass, 0, target);
     i0 = (int)s.at[0] * a.slice;
     i1 = min(i0 + a.slice, V);
     base = s.at[1];
     whole = false;
   }
-  const int wave = tid >> 6, lane = tid & 63;
-  for (; whole || i1 - i0 > kT; whole = false) {
-    const int seg = (i1 - i0 + 15) / 16, a0 = min(i0 + wave * seg, i1), a1 = min(a0 + seg, i1);
+#pragma unroll 1
+  for (;; whole = false) {
+    const int len = (i1 - i0 + kT - 1) / kT, a0 = min(i0 + tid * len, i1), a1 = min(a0 + len, i1);
     u64 m = 0;
-    for_range<T>(row, V, a0, a1, lane, 64, [&](float x, int i) {
+    for_range<T>(row, V, a0, a1, 0, 1, [&](float x, int i) {
       if (kept(x, i)) m += weight(r, x);
     });
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) m += __shfl_xor(m, d, 64);
-    __syncthreads();
-    if (lane == 0) s.wave[wave] = m;
-    __syncthreads();
     if (whole) {
-      u64 sum = 0;
-#pragma unroll
-      for (int w = 0; w < 16; ++w) sum += s.wave[w];
-      all = (double)sum;
+      all = (double)block_sum<kT>(m, s.wave);
       target = (double)u * all;
     }
-    int w = 0;
-    while (w < 15 && !((double)(base + s.wave[w]) > target)) base += s.wave[w++];
-    i0 = min(i0 + w * seg, i1);
-    i1 = min(i0 + seg, i1);
+    __syncthreads();
+    s.mass[tid] = m;
+    __syncthreads();
+    find_passing<kT>(s, s.mass, base, target);
+    i0 = min(i0 + (int)s.at[0] * len, i1);
+    i1 = min(i0 + len, i1);
+    base = s.at[1];
+    if (len == 1) break;
   }
-  const int i = i0 + tid;
-  u64 m = 0;
-  if (i < i1) {
-    const float x = to_f(row[i]);
-    if (x > -INFINITY && kept(x, i)) m = weight(r, x);
-  }
-  u64 sum;
-  const u64 upto = base + block_scan<kT>(m, s.wave, sum);
-  if ((double)upto > target && !((double)(upto - m) > target)) {
-    a.token[r0] = i;
-    if (a.prob) a.prob[r0] = (float)((double)m / all);
+  if (tid == 0) {
+    a.token[r0] = i0;
+    if (a.prob) a.prob[r0] = (float)((double)s.at[2] / all);
   }
 }
 
@@ -747,8 +770,9 @@ catq_status launch_sample(SampleArgs a, int64_t rows, hipStream_t stream) {
               hipLaunchKernelGGL((sample_first_kernel<T>), grid, dim3(kS), 0, stream, a));
   CATQ_TRACED(stream, "sample_bins_kernel", 0.0, bytes, rows, a.V, sl.n,
               hipLaunchKernelGGL((sample_bins_kernel<T>), grid, dim3(kS), 0, stream, a));
-  CATQ_TRACED(stream, "sample_gather_kernel", 0.0, bytes, rows, a.V, sl.n,
-              hipLaunchKernelGGL((sample_gather_kernel<T>), grid, dim3(kS), 0, stream, a));
+  if (a.top_k || a.top_p)     // (no row has a filter that gathers)
+    CATQ_TRACED(stream, "sample_gather_kernel", 0.0, bytes, rows, a.V, sl.n,
+                hipLaunchKernelGGL((sample_gather_kernel<T>), grid, dim3(kS), 0, stream, a));
   CATQ_TRACED(stream, "sample_kernel", 0.0, 0.0, rows, a.V, 1,
               hipLaunchKernelGGL((sample_kernel<T, true>), dim3((unsigned)rows), dim3(kT), 0, stream, a));
   CATQ_CHECK_LAUNCH("sample");
