@@ -4,19 +4,23 @@
 //   y      = res + sum_j w_j * s_j * qa_j (alpha T)^T,  qa, s the 8-bit codes and scale of slot j's a
 //
 // What a few tokens cost is the weights of the experts that they hit, read once: 2 bits each and a scale per group.
-// A wave takes rows of 16 weights and a run of 128-code chunks (or of experts), and brings up to eight chunks of their
-// codes into LDS of its own at once by direct copies, so that a unit has some 100 KB in flight without a wait between
-// waves; the matrix products take 16 token columns, of which a few are used.
+// A wave takes rows of 16 weights and a run of 128-code chunks, and brings up to eight or twelve chunks of their codes
+// into LDS of its own at once by direct copies, so that a unit has some 100 KB in flight without a wait between waves;
+// the matrix products take 16 token columns, of which a few are used.
+//
+// Launches.  Up to eight tokens: every workgroup of the first kernel finds the tokens' experts itself, and where the
+// codes of a are few every workgroup of the second forms them itself: two launches. More tokens: the experts and
+// their slots are laid out by a kernel of one workgroup, the codes by the quantizer.
 #include <type_traits>
 
 #include "kernels.h"
 #include "moe_topk.h"
+#include "quant8.h"
 #include "ternary8.h"
 
 namespace catq {
 namespace {
 
-constexpr int kBurst = 8;        // chunks of 128 codes copied at once
 constexpr int kPitch = 20;       // floats between groups of a tile's scales in LDS
 
 struct MoeArgs {
@@ -35,6 +39,8 @@ struct MoeArgs {
   float* act;             // [T][k][F]
   int8_t* qa;             // [T][k][F]
   float* sa;              // [T][k]
+  int32_t* hits;          // experts that are hit, from hits[1] on their ids, first slots and numbers of slots
+  int32_t* slots;         // [T][k], by expert
   int32_t T, E, k, h, F;
   int32_t shift;          // log2(g / 128)
 };
@@ -53,217 +59,339 @@ __device__ __forceinline__ Tile tile_at(const uint8_t* P, const float* A, int64_
   return t;
 }
 
-// LDS of a wave: for each of R tiles four copies of 1 KB ([16 rows][4 pieces of 16 bytes], piece p of row t at
-// p ^ (t / 4): two chunks) and the scales of up to eight groups
-template <int R>
+// LDS of a wave: for each of R tiles NB / 2 copies of 1 KB ([16 rows][4 pieces of 16 bytes], piece p of row t at
+// p ^ (t / 4): two chunks) and the scales of the groups of NB chunks
+constexpr int scale_slots(int NB) { return NB <= 8 ? 8 : 16; }
+template <int R, int NB>
 constexpr int own_bytes() {
-  return R * (kBurst / 2 * 1024 + 8 * kPitch * 4);
+  return R * (NB / 2 * 1024 + scale_slots(NB) * kPitch * 4);
 }
 
-// out[r][e] += sum over chunks c0 .. c1 - 1 of alpha * (codes . x): row 4 (lane / 16) + e of tile r, the column of x
-// that this lane points to. n: codes of a row.
-template <int R>
-__device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t* x, int c0, int c1, int n, int shift,
-                                             char* own, f32x4 (&out)[R]) {
+// out[r][c][e] += sum over chunks c0 .. c1 - 1 of alpha * (codes . x): row 4 (lane / 16) + e of tile r, and the column
+// of tile c that this lane points to, in memory or (XLDS) in LDS. n: codes of a row. NB chunks at a time.
+template <int R, int C, int NB>
+__device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t* const (&x)[C], int c0, int c1, int n,
+                                             int shift, char* own, f32x4 (&out)[R][C]) {
+  constexpr int G = scale_slots(NB), AU = 16 * G / 64;
   const int lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
   const int row_bytes = n >> 2, ng = n >> (7 + shift);
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)own;
-  float* s_al = reinterpret_cast<float*>(own + R * (kBurst / 2 * 1024));
+  float* s_al = reinterpret_cast<float*>(own + R * (NB / 2 * 1024));
   const uint32_t woff = (uint32_t)((lane >> 2) * row_bytes + ((lane & 3) ^ (lane >> 4)) * 16);
-  for (int b0 = c0; b0 < c1; b0 += kBurst) {
-    const int nb = min(c1 - b0, kBurst), g0 = b0 >> shift;
+  for (int b0 = c0; b0 < c1; b0 += NB) {
+    const int nb = min(c1 - b0, NB), g0 = b0 >> shift;
     wait_lds();     // what the last burst read may be written over
 #pragma unroll
-    for (int p = 0; p < kBurst / 2; ++p) {
-      if (2 * p >= nb) break;
+    for (int p = 0; p < NB / 2; ++p) {
+      if (2 * p >= nb) continue;
 #pragma unroll
       for (int r = 0; r < R; ++r)    // (past a row's end: the next row, or zeros; never used)
-        dma16_lds(tile[r].codes, woff + (uint32_t)(b0 + 2 * p) * 32u, 0u, lds + (r * (kBurst / 2) + p) * 1024);
+        dma16_lds(tile[r].codes, woff + (uint32_t)(b0 + 2 * p) * 32u, 0u, lds + (r * (NB / 2) + p) * 1024);
     }
-    float av[R][2];
+    float av[R][AU];
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int i = lane + 64 * u, g = min(g0 + (i & 7), ng - 1);
-        av[r][u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(tile[r].alpha, ((i >> 3) * ng + g) * 4, 0, 0));
+      for (int u = 0; u < AU; ++u) {
+        const int i = lane + 64 * u, g = min(g0 + i % G, ng - 1);
+        av[r][u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(tile[r].alpha, (i / G * ng + g) * 4, 0, 0));
       }
-    u32x4 xr[kBurst][2];
-#pragma unroll
-    for (int c = 0; c < kBurst; ++c) {
+    // activations, some chunks ahead
+    constexpr int PF = NB <= 8 ? NB : C == 1 ? 4 : 3;
+    u32x4 xr[PF][C][2];
+    auto load_x = [&](int c, u32x4 (&v)[C][2]) __attribute__((always_inline)) {
       const int at = min(b0 + c, c1 - 1) * 128 + 32 * q;
-      xr[c][0] = *reinterpret_cast<const u32x4*>(x + at);
-      xr[c][1] = *reinterpret_cast<const u32x4*>(x + at + 16);
-    }
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        v[j][0] = *reinterpret_cast<const u32x4*>(x[j] + at);
+        v[j][1] = *reinterpret_cast<const u32x4*>(x[j] + at + 16);
+      }
+    };
+#pragma unroll
+    for (int c = 0; c < PF; ++c) load_x(c, xr[c]);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < AU; ++u) {
         const int i = lane + 64 * u;
-        s_al[(r * 8 + (i & 7)) * kPitch + (i >> 3)] = av[r][u];
+        s_al[(r * G + i % G) * kPitch + i / G] = av[r][u];
       }
     wait_vmem();
     wait_lds();
 #pragma unroll
-    for (int c = 0; c < kBurst; ++c) {
-      if (c >= nb) break;
-      const u32x4 x0 = transpose16(xr[c][0]), x1 = transpose16(xr[c][1]);
+    for (int c = 0; c < NB; ++c) {
+      if (c >= nb) continue;
+      u32x4 xs[C][2];
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        xs[j][0] = transpose16(xr[c % PF][j][0]);
+        xs[j][1] = transpose16(xr[c % PF][j][1]);
+      }
+      if (c + PF < NB) load_x(c + PF, xr[c % PF]);
       const int g = ((b0 + c) >> shift) - g0;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const uint2 w = *reinterpret_cast<const uint2*>(own + (r * (kBurst / 2) + c / 2) * 1024 + c16 * 64 +
+        const uint2 w = *reinterpret_cast<const uint2*>(own + (r * (NB / 2) + c / 2) * 1024 + c16 * 64 +
                                                         ((2 * (c & 1) + (q >> 1)) ^ (c16 >> 2)) * 16 + 8 * (q & 1));
-        const f32x4 sc = *reinterpret_cast<const f32x4*>(&s_al[(r * 8 + g) * kPitch + 4 * q]);
-        i32x4 acc = {0, 0, 0, 0};
-        acc = mfma_i8(decode16_i8(w.x), x0, acc);
-        acc = mfma_i8(decode16_i8(w.y), x1, acc);
+        const f32x4 sc = *reinterpret_cast<const f32x4*>(&s_al[(r * G + g) * kPitch + 4 * q]);
+        const u32x4 w0 = decode16_i8(w.x), w1 = decode16_i8(w.y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[r][e] = fmaf(sc[e], (float)acc[e], out[r][e]);
+        for (int j = 0; j < C; ++j) {
+          i32x4 acc = {0, 0, 0, 0};
+          acc = mfma_i8(w0, xs[j][0], acc);
+          acc = mfma_i8(w1, xs[j][1], acc);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[r][j][e] = fmaf(sc[e], (float)acc[e], out[r][j][e]);
+        }
       }
     }
   }
 }
 
-// The experts of every token, a wave each.
-template <int PER>
-__global__ __launch_bounds__(256) void moe_experts_kernel(MoeArgs a) {
-  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (t >= a.T) return;
-  int id;
-  float w;
-  topk_token<PER>(a.logits + (int64_t)t * a.E, a.E, a.k, lane, id, w);
-  if (lane < a.k) {
-    a.ids[t * a.k + lane] = id;
-    a.w[t * a.k + lane] = w;
-  }
+__device__ __forceinline__ void topk_any(const MoeArgs& a, int t, int lane, int& id, float& w) {
+  const float* row = a.logits + (int64_t)t * a.E;
+  if (a.E <= 64) topk_token<1>(row, a.E, a.k, lane, id, w);
+  else if (a.E <= 128) topk_token<2>(row, a.E, a.k, lane, id, w);
+  else if (a.E <= 256) topk_token<4>(row, a.E, a.k, lane, id, w);
+  else topk_token<16>(row, a.E, a.k, lane, id, w);
 }
 
-// Gate, up and their product: 16 values of a for all slots of an expert. Item i is the expert of slot i, if none
-// before it has the same, or, where there are more slots than experts, expert i if any slot has it.
-constexpr int kUpWaves = 4;
-__global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
-  constexpr int OWN = own_bytes<2>();
-  __shared__ __align__(16) char s_own[kUpWaves][OWN];
-  __shared__ int s_slot[1024];
-  __shared__ int s_n, s_e;
-  static_assert(OWN >= 2 * 16 * 17 * 4, "the waves' sums fit their place");
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = a.T * a.k, item = blockIdx.y;
-  if (wave == 0) {
-    const int e = n <= a.E ? a.ids[item] : item;
-    int have = 0;
-    bool first = true;
-    for (int b = 0; b < n; b += 64) {
-      const bool mine = b + lane < n && a.ids[b + lane] == e;
-      const unsigned long long m = __ballot(mine);
-      if (n <= a.E && have == 0 && m && b + __builtin_ctzll(m) < item) {
-        first = false;
-        break;
-      }
-      if (mine) s_slot[have + __popcll(m & ((1ull << lane) - 1))] = b + lane;
-      have += __popcll(m);
-    }
-    if (lane == 0) {
-      s_n = first ? have : 0;
-      s_e = e;
+// The experts of every token, and the slots of every expert that is hit. One workgroup. (The order of an expert's
+// slots is that of LDS atomics: it decides in which column a slot is computed, and nothing else.)
+__global__ __launch_bounds__(1024) void moe_experts_kernel(MoeArgs a) {
+  __shared__ int s_count[1024], s_first[1024];
+  __shared__ int s_wave[16], s_wave_hits[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  s_count[tid] = 0;
+  __syncthreads();
+  for (int t = wave; t < a.T; t += 16) {
+    int id;
+    float w;
+    topk_any(a, t, lane, id, w);
+    if (lane < a.k) {
+      a.ids[t * a.k + lane] = id;
+      a.w[t * a.k + lane] = w;
+      atomicAdd(&s_count[id], 1);
     }
   }
   __syncthreads();
-  const int slots = __builtin_amdgcn_readfirstlane(s_n), e = __builtin_amdgcn_readfirstlane(s_e);
-  if (slots == 0) return;
+  const int c = s_count[tid];           // (thread e: expert e)
+  const unsigned long long m = __ballot(c > 0);
+  int at = c;                           // inclusive sum over the wave
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(at, d, 64);
+    if (lane >= d) at += o;
+  }
+  if (lane == 63) {
+    s_wave[wave] = at;
+    s_wave_hits[wave] = __popcll(m);
+  }
+  __syncthreads();
+  int before = 0, hit = 0, hits = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) {
+      before += s_wave[w];
+      hit += s_wave_hits[w];
+    }
+    hits += s_wave_hits[w];
+  }
+  const int first = before + at - c;
+  s_first[tid] = first;
+  if (c > 0) {
+    int32_t* h = a.hits + 1 + 3 * (hit + __popcll(m & ((1ull << lane) - 1)));
+    h[0] = tid;
+    h[1] = first;
+    h[2] = c;
+  }
+  if (tid == 0) a.hits[0] = hits;
+  __syncthreads();
+  for (int i = tid; i < a.T * a.k; i += 1024) a.slots[atomicAdd(&s_first[a.ids[i]], 1)] = i;   // (this workgroup's own writes)
+}
+
+// Gate, up and their product: 16 values of a for all slots of an expert.
+// FUSED (up to eight tokens): the workgroup finds the tokens' experts; item i is the expert of slot i, if none before it
+// has the same, or, where there are more slots than experts, expert i if any slot has it. Otherwise item i is the
+// i-th expert that is hit.
+constexpr int kUpWaves = 4, kUpBurst = 8, kFusedTokens = 8;
+template <bool FUSED>
+__global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
+  constexpr int OWN = own_bytes<2, kUpBurst>();
+  __shared__ __align__(16) char s_own[kUpWaves][OWN];
+  __shared__ int s_ids[FUSED ? kFusedTokens * 16 : 1];
+  __shared__ int s_slot[16];
+  static_assert(OWN >= 2 * 16 * 17 * 4, "the waves' sums fit their place");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int item = blockIdx.y;
+  int e, slots;
+  const int32_t* list = nullptr;
+  if constexpr (FUSED) {
+    const int n = a.T * a.k;
+    for (int t = wave; t < a.T; t += kUpWaves) {
+      int id;
+      float w;
+      topk_any(a, t, lane, id, w);
+      if (lane < a.k) {
+        s_ids[t * a.k + lane] = id;
+        if (blockIdx.x == 0 && item == 0) {
+          a.ids[t * a.k + lane] = id;
+          a.w[t * a.k + lane] = w;
+        }
+      }
+    }
+    __syncthreads();
+    e = __builtin_amdgcn_readfirstlane(n <= a.E ? s_ids[item] : item);
+    slots = 0;
+    bool first = true;
+    for (int b = 0; b < n; b += 64) {      // (at most eight slots: an expert is hit once by a token)
+      const bool mine = b + lane < n && s_ids[b + lane] == e;
+      const unsigned long long m = __ballot(mine);
+      if (n <= a.E && slots == 0 && m && b + __builtin_ctzll(m) < item) first = false;
+      if (wave == 0 && mine) s_slot[slots + __popcll(m & ((1ull << lane) - 1))] = b + lane;
+      slots += __popcll(m);
+    }
+    if (!first || slots == 0) return;
+    __syncthreads();
+  } else {
+    if (item >= a.hits[0]) return;
+    const int32_t* h = a.hits + 1 + 3 * item;
+    e = __builtin_amdgcn_readfirstlane(h[0]);
+    list = a.slots + h[1];
+    slots = __builtin_amdgcn_readfirstlane(h[2]);
+  }
   const int f0 = blockIdx.x * 16, nch = a.h >> 7;
   const int64_t row = (int64_t)e * 2 * a.F + f0;
   const Tile tile[2] = {tile_at(a.P1, a.A1, row, a.h, a.shift), tile_at(a.P1, a.A1, row + a.F, a.h, a.shift)};
   for (int s0 = 0; s0 < slots; s0 += 16) {
-    const int here = min(slots - s0, 16);
-    const int token = s_slot[s0 + min(lane & 15, here - 1)] / a.k;
-    f32x4 out[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    rows_product<2>(tile, a.X + token * a.ldx, wave * nch / kUpWaves, (wave + 1) * nch / kUpWaves, a.h, a.shift,
-                    s_own[wave], out);
+    const int here = min(slots - s0, 16), col = min(lane & 15, here - 1);
+    const int slot = FUSED ? s_slot[col] : list[s0 + col];
+    if (!FUSED && tid < here) s_slot[tid] = slot;      // (lanes 0 .. 15: column = lane)
+    f32x4 out[2][1] = {{{0.f, 0.f, 0.f, 0.f}}, {{0.f, 0.f, 0.f, 0.f}}};
+    const int8_t* const x[1] = {a.X + slot / a.k * a.ldx};
+    rows_product<2, 1, kUpBurst>(tile, x, wave * nch / kUpWaves, (wave + 1) * nch / kUpWaves, a.h, a.shift,
+                                 s_own[wave], out);
     float* red = reinterpret_cast<float*>(s_own[wave]);
     wait_lds();
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) red[(r * 16 + (lane & 15)) * 17 + 4 * (lane >> 4) + i] = out[r][i];
+      for (int i = 0; i < 4; ++i) red[(r * 16 + (lane & 15)) * 17 + 4 * (lane >> 4) + i] = out[r][0][i];
     __syncthreads();
-    for (int i = tid; i < 16 * here; i += kUpWaves * 64) {
-      const int col = i >> 4, f = i & 15;
+    if (tid < 16 * here) {
+      const int c = tid >> 4, f = tid & 15;
       float g = 0.f, u = 0.f;
 #pragma unroll
       for (int w = 0; w < kUpWaves; ++w) {
         const float* p = reinterpret_cast<const float*>(s_own[w]);
-        g += p[col * 17 + f];
-        u += p[(16 + col) * 17 + f];
+        g += p[c * 17 + f];
+        u += p[(16 + c) * 17 + f];
       }
-      const int slot = s_slot[s0 + col];
-      const float xs = a.xs[slot / a.k];
-      a.act[(int64_t)slot * a.F + f0 + f] = swiglu1(g * xs, u * xs);
+      const int sl = s_slot[c];
+      const float xs = a.xs[sl / a.k];
+      a.act[(int64_t)sl * a.F + f0 + f] = swiglu1(g * xs, u * xs);
     }
     __syncthreads();
   }
 }
 
-// Down and the sum over a token's experts: 16 outputs of 16 tokens; the waves take the experts that these hit in turn.
-constexpr int kDownWaves = 8;
-template <typename T>
+// Down and the sum over a token's experts: 16 outputs of 16 C tokens; the waves take the experts that these hit in
+// turn, or runs of their chunks where they are few.
+// FUSED: the codes of a, kFusedCodes at most, are formed here, in LDS.
+constexpr int kDownWaves = 16, kDownBurst = 12, kFusedCodes = 24 * 1024;
+template <typename T, int C, bool FUSED>
 __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs a) {
-  constexpr int OWN = own_bytes<1>();
+  constexpr int OWN = own_bytes<1, kDownBurst>(), SLOTS = 16 * 16 * C;
   __shared__ __align__(16) char s_own[kDownWaves][OWN];
-  __shared__ int s_ids[256];
-  __shared__ float s_w[256];
+  __shared__ __align__(16) int8_t s_qa[FUSED ? kFusedCodes : 16];
+  __shared__ int s_ids[SLOTS];
+  __shared__ float s_w[SLOTS];
   __shared__ unsigned int s_bits[32];
-  __shared__ short s_list[256];
-  __shared__ int s_n;
-  static_assert(OWN >= 16 * 17 * 4, "the waves' sums fit their place");
+  __shared__ short s_list[SLOTS];
+  static_assert(OWN >= C * 16 * 17 * 4, "the waves' sums fit their place");
+  static_assert(SLOTS <= kDownWaves * 64, "a slot per thread");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int t0 = blockIdx.y * 16, toks = min(a.T - t0, 16), n = toks * a.k;
+  const int t0 = blockIdx.y * 16 * C, toks = min(a.T - t0, 16 * C), n = toks * a.k;
   if (tid < 32) s_bits[tid] = 0u;
   __syncthreads();
   if (tid < n) {
     const int e = a.ids[t0 * a.k + tid];
     s_ids[tid] = e;
-    s_w[tid] = a.w[t0 * a.k + tid] * a.sa[t0 * a.k + tid];
+    s_w[tid] = FUSED ? a.w[t0 * a.k + tid] : a.w[t0 * a.k + tid] * a.sa[t0 * a.k + tid];
     atomicOr(&s_bits[e >> 5], 1u << (e & 31));
   }
   __syncthreads();
-  for (int e = tid; e < a.E; e += kDownWaves * 64) {
-    const unsigned int bits = s_bits[e >> 5];
-    if (!((bits >> (e & 31)) & 1u)) continue;
-    int at = __popc(bits & ((1u << (e & 31)) - 1u));
-    for (int w = 0; w < (e >> 5); ++w) at += __popc(s_bits[w]);
-    s_list[at] = (short)e;
+  int hit = 0;
+  for (int w = 0; w < (a.E + 31) / 32; ++w) hit += __popc(s_bits[w]);
+  if (tid < a.E) {
+    const unsigned int bits = s_bits[tid >> 5];
+    if ((bits >> (tid & 31)) & 1u) {
+      int at = __popc(bits & ((1u << (tid & 31)) - 1u));
+      for (int w = 0; w < (tid >> 5); ++w) at += __popc(s_bits[w]);
+      s_list[at] = (short)tid;
+    }
   }
-  if (tid == 0) {
-    int c = 0;
-    for (int w = 0; w < (a.E + 31) / 32; ++w) c += __popc(s_bits[w]);
-    s_n = c;
+  if constexpr (FUSED) {
+    for (int i = wave; i < n; i += kDownWaves) {
+      const float* p = a.act + (int64_t)(t0 * a.k + i) * a.F;
+      unsigned int m = 0u;
+      for (int f = 4 * lane; f < a.F; f += 256) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(p + f);
+        m = max(max(m, max(mag_bits(v[0]), mag_bits(v[1]))), max(mag_bits(v[2]), mag_bits(v[3])));
+      }
+      const float s = quant8_scale(wave_umax(m));
+      if (lane == 0) s_w[i] *= s;
+      for (int f = 4 * lane; f < a.F; f += 256) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(p + f);
+        float v[4] = {x[0], x[1], x[2], x[3]};
+        quant8_n(v, s);
+        *reinterpret_cast<unsigned int*>(s_qa + i * a.F + f) = pack_codes(v[0], v[1], v[2], v[3]);
+      }
+    }
   }
   __syncthreads();
-  const int r0 = blockIdx.x * 16, c16 = lane & 15, hit = s_n;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i = wave; i < hit; i += kDownWaves) {
-    const int e = __builtin_amdgcn_readfirstlane((int)s_list[i]);
-    int slot = -1, any = 0;
-    for (int j = 0; j < a.k; ++j)
-      if (c16 < toks && s_ids[c16 * a.k + j] == e) slot = c16 * a.k + j;
-    const unsigned long long m = __ballot(slot >= 0);
-    any = __shfl(slot, __builtin_ctzll(m), 64);      // (the other columns repeat one that is used)
-    const float f = slot >= 0 ? s_w[slot] : 0.f;
-    const Tile tile[1] = {tile_at(a.P2, a.A2, (int64_t)e * a.h + r0, a.F, a.shift)};
-    f32x4 out[1] = {{0.f, 0.f, 0.f, 0.f}};
-    rows_product<1>(tile, a.qa + (int64_t)(t0 * a.k + (slot >= 0 ? slot : any)) * a.F, 0, a.F >> 7, a.F, a.shift,
-                    s_own[wave], out);
+  const int r0 = blockIdx.x * 16, c16 = lane & 15, nch = a.F >> 7;
+  int parts = 1;
+  while (hit * parts < kDownWaves && 2 * parts <= nch) parts *= 2;
+  f32x4 sum[C];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sum[j] = slot >= 0 ? fmaf(f, out[0][j], sum[j]) : sum[j];
+  for (int j = 0; j < C; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = wave; i < hit * parts; i += kDownWaves) {
+    const int e = __builtin_amdgcn_readfirstlane((int)s_list[i / parts]), part = i % parts;
+    int slot[C], any = -1;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int t = 16 * j + c16;
+      slot[j] = -1;
+      for (int u = 0; u < a.k; ++u)
+        if (t < toks && s_ids[t * a.k + u] == e) slot[j] = t * a.k + u;
+      any = max(any, slot[j]);
+    }
+    any = __shfl(any, __builtin_ctzll(__ballot(any >= 0)), 64);   // (the other columns repeat one that is used)
+    const Tile tile[1] = {tile_at(a.P2, a.A2, (int64_t)e * a.h + r0, a.F, a.shift)};
+    f32x4 out[1][C];
+    const int8_t* x[C];
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      out[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int sl = slot[j] >= 0 ? slot[j] : any;
+      x[j] = FUSED ? s_qa + sl * a.F : a.qa + (int64_t)(t0 * a.k + sl) * a.F;
+    }
+    rows_product<1, C, kDownBurst>(tile, x, part * nch / parts, (part + 1) * nch / parts, a.F, a.shift, s_own[wave], out);
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const float f = slot[j] >= 0 ? s_w[slot[j]] : 0.f;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) sum[j][v] = slot[j] >= 0 ? fmaf(f, out[0][j][v], sum[j][v]) : sum[j][v];
+    }
   }
   wait_lds();
   float* red = reinterpret_cast<float*>(s_own[wave]);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) red[c16 * 17 + 4 * (lane >> 4) + j] = sum[j];
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) red[(16 * j + c16) * 17 + 4 * (lane >> 4) + v] = sum[j][v];
   __syncthreads();
-  for (int i = tid; i < 16 * toks; i += kDownWaves * 64) {
-    const int col = i >> 4, r = i & 15;
+  if (tid < 16 * toks) {
+    const int col = tid >> 4, r = tid & 15;
     const int64_t at = (int64_t)(t0 + col) * a.h + r0 + r;
     float v = 0.f;
 #pragma unroll
@@ -289,7 +417,7 @@ catq_status moe_check(const catq_moe_desc* d, int64_t T) {
 }
 
 struct MoeSpace {
-  size_t ids, w, sa, qa, act, end;
+  size_t ids, w, sa, hits, slots, qa, act, end;
 };
 MoeSpace moe_space(const catq_moe_desc* d, int64_t T) {
   const size_t n = (size_t)T * d->top_k;
@@ -297,7 +425,9 @@ MoeSpace moe_space(const catq_moe_desc* d, int64_t T) {
   s.ids = 0;
   s.w = round_up(n * 4, 256);
   s.sa = s.w + round_up(n * 4, 256);
-  s.qa = s.sa + round_up(n * 4, 256);
+  s.hits = s.sa + round_up(n * 4, 256);
+  s.slots = s.hits + round_up((1 + 3 * (size_t)d->n_experts) * 4, 256);
+  s.qa = s.slots + round_up(n * 4, 256);
   s.act = s.qa + round_up(n * d->ffn, 256);
   s.end = s.act + round_up(n * d->ffn * 4, 256);
   return s;
@@ -338,27 +468,33 @@ extern "C" catq_status catq_ternary_moe_a8(const catq_moe_desc* d, const float* 
   MoeArgs a{logits, q, x_scale, ldq, gu_packed, gu_alpha, down_packed, down_alpha, res, y,
             reinterpret_cast<int32_t*>(ws + sp.ids), reinterpret_cast<float*>(ws + sp.w),
             reinterpret_cast<float*>(ws + sp.act), reinterpret_cast<int8_t*>(ws + sp.qa),
-            reinterpret_cast<float*>(ws + sp.sa), (int32_t)T, d->n_experts, d->top_k, d->hidden, d->ffn,
+            reinterpret_cast<float*>(ws + sp.sa), reinterpret_cast<int32_t*>(ws + sp.hits),
+            reinterpret_cast<int32_t*>(ws + sp.slots), (int32_t)T, d->n_experts, d->top_k, d->hidden, d->ffn,
             __builtin_ctz((unsigned)d->group_size / 128)};
   const int n = (int)T * a.k, hit = n < a.E ? n : a.E;
   const double wt = (double)hit * a.h * a.F * (0.25 + 4.0 / d->group_size);
-  auto experts = [&](auto kernel) {
+  const bool fused = T <= kFusedTokens, codes_here = T <= 16 && (int64_t)n * a.F <= kFusedCodes;
+  if (!fused) {
     CATQ_TRACED(stream, "moe_experts_kernel", 0.0, 4.0 * T * a.E, T, a.E, a.k,
-                hipLaunchKernelGGL(kernel, dim3((unsigned)((T + 3) / 4)), dim3(256), 0, stream, a));
-  };
-  if (a.E <= 64) experts(moe_experts_kernel<1>);
-  else if (a.E <= 128) experts(moe_experts_kernel<2>);
-  else if (a.E <= 256) experts(moe_experts_kernel<4>);
-  else experts(moe_experts_kernel<16>);
-  CATQ_TRACED(stream, "moe_up_kernel", 4.0 * n * a.h * a.F, 2.0 * wt, n, 2 * a.F, a.h,
-              hipLaunchKernelGGL(moe_up_kernel, dim3((unsigned)(a.F / 16), (unsigned)hit), dim3(kUpWaves * 64), 0,
-                                 stream, a));
+                hipLaunchKernelGGL(moe_experts_kernel, dim3(1), dim3(1024), 0, stream, a));
+    CATQ_CHECK_LAUNCH("moe experts");
+  }
+  auto up = fused ? moe_up_kernel<true> : moe_up_kernel<false>;
+  CATQ_TRACED(stream, fused ? "moe_up_kernel<fused>" : "moe_up_kernel", 4.0 * n * a.h * a.F, 2.0 * wt, n, 2 * a.F, a.h,
+              hipLaunchKernelGGL(up, dim3((unsigned)(a.F / 16), (unsigned)hit), dim3(kUpWaves * 64), 0, stream, a));
   CATQ_CHECK_LAUNCH("moe gate and up");
-  CATQ_TRY(catq_aux_act_quant8(a.act, CATQ_F32, n, a.F, a.F, a.qa, a.sa, stream));
-  auto down = y_dtype == CATQ_F32 ? moe_down_kernel<float> : moe_down_kernel<bf16>;
-  CATQ_TRACED(stream, "moe_down_kernel", 2.0 * n * a.h * a.F, wt, n, a.h, a.F,
-              hipLaunchKernelGGL(down, dim3((unsigned)(a.h / 16), (unsigned)((T + 15) / 16)), dim3(kDownWaves * 64), 0,
-                                 stream, a));
+  if (!codes_here) CATQ_TRY(catq_aux_act_quant8(a.act, CATQ_F32, n, a.F, a.F, a.qa, a.sa, stream));
+  const int cols = T > 16 ? 32 : 16;
+  auto down = [&](auto out) {
+    using Out = decltype(out);
+    auto kernel = codes_here ? moe_down_kernel<Out, 1, true> : cols == 16 ? moe_down_kernel<Out, 1, false>
+                                                                         : moe_down_kernel<Out, 2, false>;
+    CATQ_TRACED(stream, "moe_down_kernel", 2.0 * n * a.h * a.F, wt, n, a.h, a.F,
+                hipLaunchKernelGGL(kernel, dim3((unsigned)(a.h / 16), (unsigned)((T + cols - 1) / cols)),
+                                   dim3(kDownWaves * 64), 0, stream, a));
+  };
+  if (y_dtype == CATQ_F32) down(float{});
+  else down(bf16{});
   CATQ_CHECK_LAUNCH("moe down");
   return CATQ_OK;
 }
