@@ -8,7 +8,7 @@
 // into LDS of its own at once by direct copies, so that a unit has some 100 KB in flight without a wait between waves;
 // the matrix products take 16 token columns, of which a few are used.
 //
-// Launches.  Up to eight tokens: every workgroup of the first kernel finds the tokens' experts itself, and where the
+// Launches.  Up to four tokens: every workgroup of the first kernel finds the tokens' experts itself, and where the
 // codes of a are few every workgroup of the second forms them itself: two launches. More tokens: the experts and
 // their slots are laid out by a kernel of one workgroup, the codes by the quantizer.
 #include <type_traits>
@@ -67,11 +67,11 @@ constexpr int own_bytes() {
   return R * (NB / 2 * 1024 + scale_slots(NB) * kPitch * 4);
 }
 
-// out[r][c][e] += sum over chunks c0 .. c1 - 1 of alpha * (codes . x): row 4 (lane / 16) + e of tile r, and the column
-// of tile c that this lane points to, in memory or (XLDS) in LDS. n: codes of a row. NB chunks at a time.
-template <int R, int C, int NB>
-__device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t* const (&x)[C], int c0, int c1, int n,
-                                             int shift, char* own, f32x4 (&out)[R][C]) {
+// out[r][e] += sum over chunks c0 .. c1 - 1 of alpha * (codes . x): row 4 (lane / 16) + e of tile r, and the column
+// that this lane points to, if it is used (the others' results are nothing). n: codes of a row. NB chunks at a time.
+template <int R, int NB>
+__device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t* x, bool used, int c0, int c1, int n,
+                                             int shift, char* own, f32x4 (&out)[R]) {
   constexpr int G = scale_slots(NB), AU = 16 * G / 64;
   const int lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
   const int row_bytes = n >> 2, ng = n >> (7 + shift);
@@ -96,19 +96,18 @@ __device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t
         const int i = lane + 64 * u, g = min(g0 + i % G, ng - 1);
         av[r][u] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(tile[r].alpha, (i / G * ng + g) * 4, 0, 0));
       }
-    // activations, some chunks ahead
-    constexpr int PF = NB <= 8 ? NB : C == 1 ? 4 : 3;
-    u32x4 xr[PF][C][2];
-    auto load_x = [&](int c, u32x4 (&v)[C][2]) __attribute__((always_inline)) {
+    // activations, some chunks ahead (only where a column is used: a load takes the L1 as long as it has lanes)
+    constexpr int PF = NB <= 8 ? NB : 6;
+    u32x4 xr[PF][2];
+    auto load_x = [&](int c, u32x4 (&v)[2]) __attribute__((always_inline)) {
       const int at = min(b0 + c, c1 - 1) * 128 + 32 * q;
-#pragma unroll
-      for (int j = 0; j < C; ++j) {
-        v[j][0] = *reinterpret_cast<const u32x4*>(x[j] + at);
-        v[j][1] = *reinterpret_cast<const u32x4*>(x[j] + at + 16);
-      }
+      v[0] = *reinterpret_cast<const u32x4*>(x + at);
+      v[1] = *reinterpret_cast<const u32x4*>(x + at + 16);
     };
+    if (used) {
 #pragma unroll
-    for (int c = 0; c < PF; ++c) load_x(c, xr[c]);
+      for (int c = 0; c < PF; ++c) load_x(c, xr[c]);
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -121,28 +120,19 @@ __device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
       if (c >= nb) continue;
-      u32x4 xs[C][2];
-#pragma unroll
-      for (int j = 0; j < C; ++j) {
-        xs[j][0] = transpose16(xr[c % PF][j][0]);
-        xs[j][1] = transpose16(xr[c % PF][j][1]);
-      }
-      if (c + PF < NB) load_x(c + PF, xr[c % PF]);
+      const u32x4 x0 = transpose16(xr[c % PF][0]), x1 = transpose16(xr[c % PF][1]);
+      if (c + PF < NB && used) load_x(c + PF, xr[c % PF]);
       const int g = ((b0 + c) >> shift) - g0;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const uint2 w = *reinterpret_cast<const uint2*>(own + (r * (NB / 2) + c / 2) * 1024 + c16 * 64 +
                                                         ((2 * (c & 1) + (q >> 1)) ^ (c16 >> 2)) * 16 + 8 * (q & 1));
         const f32x4 sc = *reinterpret_cast<const f32x4*>(&s_al[(r * G + g) * kPitch + 4 * q]);
-        const u32x4 w0 = decode16_i8(w.x), w1 = decode16_i8(w.y);
+        i32x4 acc = {0, 0, 0, 0};
+        acc = mfma_i8(decode16_i8(w.x), x0, acc);
+        acc = mfma_i8(decode16_i8(w.y), x1, acc);
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-          i32x4 acc = {0, 0, 0, 0};
-          acc = mfma_i8(w0, xs[j][0], acc);
-          acc = mfma_i8(w1, xs[j][1], acc);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[r][j][e] = fmaf(sc[e], (float)acc[e], out[r][j][e]);
-        }
+        for (int e = 0; e < 4; ++e) out[r][e] = fmaf(sc[e], (float)acc[e], out[r][e]);
       }
     }
   }
@@ -209,10 +199,10 @@ __global__ __launch_bounds__(1024) void moe_experts_kernel(MoeArgs a) {
 }
 
 // Gate, up and their product: 16 values of a for all slots of an expert.
-// FUSED (up to eight tokens): the workgroup finds the tokens' experts; item i is the expert of slot i, if none before it
+// FUSED (a token per wave): the workgroup finds the tokens' experts; item i is the expert of slot i, if none before it
 // has the same, or, where there are more slots than experts, expert i if any slot has it. Otherwise item i is the
 // i-th expert that is hit.
-constexpr int kUpWaves = 4, kUpBurst = 8, kFusedTokens = 8;
+constexpr int kUpWaves = 4, kUpBurst = 8, kFusedTokens = kUpWaves;
 template <bool FUSED>
 __global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
   constexpr int OWN = own_bytes<2, kUpBurst>();
@@ -242,7 +232,7 @@ __global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
     e = __builtin_amdgcn_readfirstlane(n <= a.E ? s_ids[item] : item);
     slots = 0;
     bool first = true;
-    for (int b = 0; b < n; b += 64) {      // (at most eight slots: an expert is hit once by a token)
+    for (int b = 0; b < n; b += 64) {      // (an expert is hit once by a token)
       const bool mine = b + lane < n && s_ids[b + lane] == e;
       const unsigned long long m = __ballot(mine);
       if (n <= a.E && slots == 0 && m && b + __builtin_ctzll(m) < item) first = false;
@@ -265,16 +255,15 @@ __global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
     const int here = min(slots - s0, 16), col = min(lane & 15, here - 1);
     const int slot = FUSED ? s_slot[col] : list[s0 + col];
     if (!FUSED && tid < here) s_slot[tid] = slot;      // (lanes 0 .. 15: column = lane)
-    f32x4 out[2][1] = {{{0.f, 0.f, 0.f, 0.f}}, {{0.f, 0.f, 0.f, 0.f}}};
-    const int8_t* const x[1] = {a.X + slot / a.k * a.ldx};
-    rows_product<2, 1, kUpBurst>(tile, x, wave * nch / kUpWaves, (wave + 1) * nch / kUpWaves, a.h, a.shift,
-                                 s_own[wave], out);
+    f32x4 out[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    rows_product<2, kUpBurst>(tile, a.X + slot / a.k * a.ldx, (lane & 15) < here, wave * nch / kUpWaves,
+                              (wave + 1) * nch / kUpWaves, a.h, a.shift, s_own[wave], out);
     float* red = reinterpret_cast<float*>(s_own[wave]);
     wait_lds();
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) red[(r * 16 + (lane & 15)) * 17 + 4 * (lane >> 4) + i] = out[r][0][i];
+      for (int i = 0; i < 4; ++i) red[(r * 16 + (lane & 15)) * 17 + 4 * (lane >> 4) + i] = out[r][i];
     __syncthreads();
     if (tid < 16 * here) {
       const int c = tid >> 4, f = tid & 15;
@@ -293,24 +282,26 @@ __global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
   }
 }
 
-// Down and the sum over a token's experts: 16 outputs of 16 C tokens; the waves take the experts that these hit in
-// turn, or runs of their chunks where they are few.
+// Down and the sum over a token's experts: 16 outputs of TG tokens. The waves take the experts that these hit in turn,
+// or runs of their chunks where they are few, 16 of an expert's slots at a time, and add to sums of their own in LDS.
 // FUSED: the codes of a, kFusedCodes at most, are formed here, in LDS.
 constexpr int kDownWaves = 16, kDownBurst = 12, kFusedCodes = 24 * 1024;
-template <typename T, int C, bool FUSED>
+template <typename T, int TG, bool FUSED>
 __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs a) {
-  constexpr int OWN = own_bytes<1, kDownBurst>(), SLOTS = 16 * 16 * C;
+  constexpr int OWN = own_bytes<1, kDownBurst>(), SLOTS = 16 * TG;
   __shared__ __align__(16) char s_own[kDownWaves][OWN];
   __shared__ __align__(16) int8_t s_qa[FUSED ? kFusedCodes : 16];
+  __shared__ float s_sum[kDownWaves][TG][17];
   __shared__ int s_ids[SLOTS];
   __shared__ float s_w[SLOTS];
+  __shared__ short s_col[kDownWaves][TG];
   __shared__ unsigned int s_bits[32];
   __shared__ short s_list[SLOTS];
-  static_assert(OWN >= C * 16 * 17 * 4, "the waves' sums fit their place");
   static_assert(SLOTS <= kDownWaves * 64, "a slot per thread");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int t0 = blockIdx.y * 16 * C, toks = min(a.T - t0, 16 * C), n = toks * a.k;
+  const int t0 = blockIdx.y * TG, toks = min(a.T - t0, TG), n = toks * a.k;
   if (tid < 32) s_bits[tid] = 0u;
+  for (int i = lane; i < TG * 17; i += 64) s_sum[wave][0][i] = 0.f;
   __syncthreads();
   if (tid < n) {
     const int e = a.ids[t0 * a.k + tid];
@@ -351,51 +342,37 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs a) {
   const int r0 = blockIdx.x * 16, c16 = lane & 15, nch = a.F >> 7;
   int parts = 1;
   while (hit * parts < kDownWaves && 2 * parts <= nch) parts *= 2;
-  f32x4 sum[C];
-#pragma unroll
-  for (int j = 0; j < C; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int i = wave; i < hit * parts; i += kDownWaves) {
     const int e = __builtin_amdgcn_readfirstlane((int)s_list[i / parts]), part = i % parts;
-    int slot[C], any = -1;
-#pragma unroll
-    for (int j = 0; j < C; ++j) {
-      const int t = 16 * j + c16;
-      slot[j] = -1;
-      for (int u = 0; u < a.k; ++u)
-        if (t < toks && s_ids[t * a.k + u] == e) slot[j] = t * a.k + u;
-      any = max(any, slot[j]);
+    int slots = 0;
+    for (int b = 0; b < n; b += 64) {
+      const bool mine = b + lane < n && s_ids[b + lane] == e;
+      const unsigned long long m = __ballot(mine);
+      if (mine) s_col[wave][slots + __popcll(m & ((1ull << lane) - 1))] = (short)(b + lane);
+      slots += __popcll(m);
     }
-    any = __shfl(any, __builtin_ctzll(__ballot(any >= 0)), 64);   // (the other columns repeat one that is used)
     const Tile tile[1] = {tile_at(a.P2, a.A2, (int64_t)e * a.h + r0, a.F, a.shift)};
-    f32x4 out[1][C];
-    const int8_t* x[C];
+    for (int c0 = 0; c0 < slots; c0 += 16) {
+      const bool used = c0 + c16 < slots;
+      const int slot = used ? (int)s_col[wave][c0 + c16] : 0;
+      f32x4 out[1] = {{0.f, 0.f, 0.f, 0.f}};
+      rows_product<1, kDownBurst>(tile, FUSED ? s_qa + slot * a.F : a.qa + (int64_t)(t0 * a.k + slot) * a.F, used,
+                                  part * nch / parts, (part + 1) * nch / parts, a.F, a.shift, s_own[wave], out);
+      if (used) {
+        float* p = &s_sum[wave][slot / a.k][4 * (lane >> 4)];
+        const float f = s_w[slot];
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      out[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const int sl = slot[j] >= 0 ? slot[j] : any;
-      x[j] = FUSED ? s_qa + sl * a.F : a.qa + (int64_t)(t0 * a.k + sl) * a.F;
-    }
-    rows_product<1, C, kDownBurst>(tile, x, part * nch / parts, (part + 1) * nch / parts, a.F, a.shift, s_own[wave], out);
-#pragma unroll
-    for (int j = 0; j < C; ++j) {
-      const float f = slot[j] >= 0 ? s_w[slot[j]] : 0.f;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) sum[j][v] = slot[j] >= 0 ? fmaf(f, out[0][j][v], sum[j][v]) : sum[j][v];
+        for (int v = 0; v < 4; ++v) p[v] = fmaf(f, out[0][v], p[v]);
+      }
     }
   }
-  wait_lds();
-  float* red = reinterpret_cast<float*>(s_own[wave]);
-#pragma unroll
-  for (int j = 0; j < C; ++j)
-#pragma unroll
-    for (int v = 0; v < 4; ++v) red[(16 * j + c16) * 17 + 4 * (lane >> 4) + v] = sum[j][v];
   __syncthreads();
   if (tid < 16 * toks) {
     const int col = tid >> 4, r = tid & 15;
     const int64_t at = (int64_t)(t0 + col) * a.h + r0 + r;
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kDownWaves; ++w) v += reinterpret_cast<const float*>(s_own[w])[col * 17 + r];
+    for (int w = 0; w < kDownWaves; ++w) v += s_sum[w][col][r];
     if (a.res) v += to_f(static_cast<const T*>(a.res)[at]);
     static_cast<T*>(a.Y)[at] = (T)v;
   }
@@ -473,7 +450,7 @@ extern "C" catq_status catq_ternary_moe_a8(const catq_moe_desc* d, const float* 
             __builtin_ctz((unsigned)d->group_size / 128)};
   const int n = (int)T * a.k, hit = n < a.E ? n : a.E;
   const double wt = (double)hit * a.h * a.F * (0.25 + 4.0 / d->group_size);
-  const bool fused = T <= kFusedTokens, codes_here = T <= 16 && (int64_t)n * a.F <= kFusedCodes;
+  const bool fused = T <= kFusedTokens, codes_here = T <= 8 && (int64_t)n * a.F <= kFusedCodes;
   if (!fused) {
     CATQ_TRACED(stream, "moe_experts_kernel", 0.0, 4.0 * T * a.E, T, a.E, a.k,
                 hipLaunchKernelGGL(moe_experts_kernel, dim3(1), dim3(1024), 0, stream, a));
@@ -487,8 +464,8 @@ extern "C" catq_status catq_ternary_moe_a8(const catq_moe_desc* d, const float* 
   const int cols = T > 16 ? 32 : 16;
   auto down = [&](auto out) {
     using Out = decltype(out);
-    auto kernel = codes_here ? moe_down_kernel<Out, 1, true> : cols == 16 ? moe_down_kernel<Out, 1, false>
-                                                                         : moe_down_kernel<Out, 2, false>;
+    auto kernel = codes_here ? moe_down_kernel<Out, 8, true> : cols == 16 ? moe_down_kernel<Out, 16, false>
+                                                                          : moe_down_kernel<Out, 32, false>;
     CATQ_TRACED(stream, "moe_down_kernel", 2.0 * n * a.h * a.F, wt, n, a.h, a.F,
                 hipLaunchKernelGGL(kernel, dim3((unsigned)(a.h / 16), (unsigned)((T + cols - 1) / cols)),
                                    dim3(kDownWaves * 64), 0, stream, a));
