@@ -6,11 +6,11 @@
 // What a few tokens cost is the weights of the experts that they hit, read once: 2 bits each and a scale per group.
 // A wave takes rows of 16 weights and a run of 128-code chunks, and brings up to eight or twelve chunks of their codes
 // into LDS of its own at once by direct copies, so that a unit has some 100 KB in flight without a wait between waves;
-// the matrix products take 16 token columns, of which a few are used.
+// the matrix products take 16 slots, of which a few are used.
 //
 // Launches.  Up to four tokens: every workgroup of the first kernel finds the tokens' experts itself, and where the
 // codes of a are few every workgroup of the second forms them itself: two launches. More tokens: the experts and
-// their slots are laid out by a kernel of one workgroup, the codes by the quantizer.
+// their slots are laid out by a kernel of their own, and so are the codes.
 #include <type_traits>
 
 #include "kernels.h"
@@ -20,8 +20,6 @@
 
 namespace catq {
 namespace {
-
-constexpr int kPitch = 20;       // floats between groups of a tile's scales in LDS
 
 struct MoeArgs {
   const float* logits;
@@ -37,8 +35,9 @@ struct MoeArgs {
   int32_t* ids;           // [T][k]
   float* w;               // [T][k]
   float* act;             // [T][k][F]
-  int8_t* qa;             // [T][k][F]
+  int8_t* qa;             // [T][k][F], in the order of matrix operands
   float* sa;              // [T][k]
+  int8_t* xt;             // [T][h]: q in the order of matrix operands
   int32_t* hits;          // experts that are hit, from hits[1] on their ids, first slots and numbers of slots
   int32_t* slots;         // [T][k], by expert
   int32_t T, E, k, h, F;
@@ -64,14 +63,20 @@ __device__ __forceinline__ Tile tile_at(const uint8_t* P, const float* A, int64_
 constexpr int scale_slots(int NB) { return NB <= 8 ? 8 : 16; }
 template <int R, int NB>
 constexpr int own_bytes() {
-  return R * (NB / 2 * 1024 + scale_slots(NB) * kPitch * 4);
+  return R * (NB / 2 * 1024 + scale_slots(NB) * 64);
 }
 
-// out[r][e] += sum over chunks c0 .. c1 - 1 of alpha * (codes . x): row 4 (lane / 16) + e of tile r, and the column
-// that this lane points to, if it is used (the others' results are nothing). n: codes of a row. NB chunks at a time.
-template <int R, int NB>
-__device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t* x, bool used, int c0, int c1, int n,
-                                             int shift, char* own, f32x4 (&out)[R]) {
+// Up to 16 slots' activations are the rows of a product, a tile's 16 weight rows its columns. Slot i is row
+// 4 (i % 4) + i / 4, so that its sums are element i / 4 of the lanes of group i % 4: with up to four slots only the first
+// element of every lane is converted and scaled.
+__device__ __forceinline__ int slot_of_row(int row) { return 4 * (row & 3) + (row >> 2); }
+
+// out[r][e] += sum over chunks c0 .. c1 - 1 of alpha * (codes . x) of weight row lane % 16 of tile r and slot
+// 4 e + lane / 16, e < ne. x: the activations of this lane's row, if it has a slot. n: codes of a row. NB chunks at a
+// time. ORDERED: the activations are in the order of the operands.
+template <int R, int NB, bool ORDERED>
+__device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t* x, bool used, int ne, int c0, int c1,
+                                             int n, int shift, char* own, f32x4 (&out)[R]) {
   constexpr int G = scale_slots(NB), AU = 16 * G / 64;
   const int lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
   const int row_bytes = n >> 2, ng = n >> (7 + shift);
@@ -113,26 +118,30 @@ __device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t
 #pragma unroll
       for (int u = 0; u < AU; ++u) {
         const int i = lane + 64 * u;
-        s_al[(r * G + i % G) * kPitch + i / G] = av[r][u];
+        s_al[(r * G + i % G) * 16 + i / G] = av[r][u];
       }
     wait_vmem();
     wait_lds();
 #pragma unroll
     for (int c = 0; c < NB; ++c) {
       if (c >= nb) continue;
-      const u32x4 x0 = transpose16(xr[c % PF][0]), x1 = transpose16(xr[c % PF][1]);
+      const u32x4 x0 = ORDERED ? xr[c % PF][0] : transpose16(xr[c % PF][0]);
+      const u32x4 x1 = ORDERED ? xr[c % PF][1] : transpose16(xr[c % PF][1]);
       if (c + PF < NB && used) load_x(c + PF, xr[c % PF]);
       const int g = ((b0 + c) >> shift) - g0;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const uint2 w = *reinterpret_cast<const uint2*>(own + (r * (NB / 2) + c / 2) * 1024 + c16 * 64 +
                                                         ((2 * (c & 1) + (q >> 1)) ^ (c16 >> 2)) * 16 + 8 * (q & 1));
-        const f32x4 sc = *reinterpret_cast<const f32x4*>(&s_al[(r * G + g) * kPitch + 4 * q]);
+        const float sc = s_al[(r * G + g) * 16 + c16];
         i32x4 acc = {0, 0, 0, 0};
-        acc = mfma_i8(decode16_i8(w.x), x0, acc);
-        acc = mfma_i8(decode16_i8(w.y), x1, acc);
+        acc = mfma_i8(x0, decode16_i8(w.x), acc);
+        acc = mfma_i8(x1, decode16_i8(w.y), acc);
+        out[r][0] = fmaf(sc, (float)acc[0], out[r][0]);
+        if (ne > 1) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[r][e] = fmaf(sc[e], (float)acc[e], out[r][e]);
+          for (int e = 1; e < 4; ++e) out[r][e] = fmaf(sc, (float)acc[e], out[r][e]);
+        }
       }
     }
   }
@@ -146,12 +155,23 @@ __device__ __forceinline__ void topk_any(const MoeArgs& a, int t, int lane, int&
   else topk_token<16>(row, a.E, a.k, lane, id, w);
 }
 
-// The experts of every token, and the slots of every expert that is hit. One workgroup. (The order of an expert's
-// slots is that of LDS atomics: it decides in which column a slot is computed, and nothing else.)
+// The first workgroup: the experts of every token, and the slots of every expert that is hit. (The order of an
+// expert's slots is that of LDS atomics: it decides in which row a slot is computed, and nothing else.)
+// The others: the activations in the order of the operands.
+constexpr int kListed = 4096;    // slots whose experts are kept in LDS
 __global__ __launch_bounds__(1024) void moe_experts_kernel(MoeArgs a) {
   __shared__ int s_count[1024], s_first[1024];
   __shared__ int s_wave[16], s_wave_hits[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ short s_ids[kListed];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.T * a.k;
+  if (blockIdx.x > 0) {
+    const int i = (blockIdx.x - 1) * 1024 + tid, per = a.h >> 4;
+    if (i >= a.T * per) return;
+    const int t = i / per, p = i - t * per;
+    *reinterpret_cast<u32x4*>(a.xt + (int64_t)t * a.h + 16 * p) =
+        transpose16(*reinterpret_cast<const u32x4*>(a.X + t * a.ldx + 16 * p));
+    return;
+  }
   s_count[tid] = 0;
   __syncthreads();
   for (int t = wave; t < a.T; t += 16) {
@@ -159,8 +179,10 @@ __global__ __launch_bounds__(1024) void moe_experts_kernel(MoeArgs a) {
     float w;
     topk_any(a, t, lane, id, w);
     if (lane < a.k) {
-      a.ids[t * a.k + lane] = id;
-      a.w[t * a.k + lane] = w;
+      const int i = t * a.k + lane;
+      a.ids[i] = id;
+      a.w[i] = w;
+      if (i < kListed) s_ids[i] = (short)id;
       atomicAdd(&s_count[id], 1);
     }
   }
@@ -195,7 +217,44 @@ __global__ __launch_bounds__(1024) void moe_experts_kernel(MoeArgs a) {
   }
   if (tid == 0) a.hits[0] = hits;
   __syncthreads();
-  for (int i = tid; i < a.T * a.k; i += 1024) a.slots[atomicAdd(&s_first[a.ids[i]], 1)] = i;   // (this workgroup's own writes)
+  for (int i = tid; i < n; i += 1024) {
+    const int id = i < kListed ? (int)s_ids[i] : a.ids[i];      // (this workgroup's own writes)
+    a.slots[atomicAdd(&s_first[id], 1)] = i;
+  }
+}
+
+// Values f .. f + 15 of a slot's a: their largest magnitude (as bits), and their codes in the order of the operands.
+__device__ __forceinline__ unsigned int mag_16(const float* p) {
+  unsigned int m = 0u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p + 4 * j);
+    m = max(max(m, max(mag_bits(v[0]), mag_bits(v[1]))), max(mag_bits(v[2]), mag_bits(v[3])));
+  }
+  return m;
+}
+__device__ __forceinline__ u32x4 codes_16(const float* p, float s) {
+  u32x4 c;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(p + 4 * j);
+    float v[4] = {x[0], x[1], x[2], x[3]};
+    quant8_n(v, s);
+    c[j] = pack_codes(v[0], v[1], v[2], v[3]);
+  }
+  return transpose16(c);
+}
+// The codes and scales of a, a wave a slot, as the quantizer forms them.
+__global__ __launch_bounds__(256) void moe_codes_kernel(MoeArgs a) {
+  const int slot = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (slot >= a.T * a.k) return;
+  const float* p = a.act + (int64_t)slot * a.F;
+  unsigned int m = 0u;
+  for (int f = 16 * lane; f < a.F; f += 1024) m = max(m, mag_16(p + f));
+  const float s = quant8_scale(wave_umax(m));
+  if (lane == 0) a.sa[slot] = s;
+  for (int f = 16 * lane; f < a.F; f += 1024)
+    *reinterpret_cast<u32x4*>(a.qa + (int64_t)slot * a.F + f) = codes_16(p + f, s);
 }
 
 // Gate, up and their product: 16 values of a for all slots of an expert.
@@ -252,18 +311,20 @@ __global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
   const int64_t row = (int64_t)e * 2 * a.F + f0;
   const Tile tile[2] = {tile_at(a.P1, a.A1, row, a.h, a.shift), tile_at(a.P1, a.A1, row + a.F, a.h, a.shift)};
   for (int s0 = 0; s0 < slots; s0 += 16) {
-    const int here = min(slots - s0, 16), col = min(lane & 15, here - 1);
-    const int slot = FUSED ? s_slot[col] : list[s0 + col];
-    if (!FUSED && tid < here) s_slot[tid] = slot;      // (lanes 0 .. 15: column = lane)
+    const int here = min(slots - s0, 16), mine = slot_of_row(lane & 15);
+    if (!FUSED && tid < here) s_slot[tid] = list[s0 + tid];
+    const bool used = mine < here;
+    const int slot = !used ? 0 : FUSED ? s_slot[mine] : list[s0 + mine];
+    const int t = slot / a.k;
     f32x4 out[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    rows_product<2, kUpBurst>(tile, a.X + slot / a.k * a.ldx, (lane & 15) < here, wave * nch / kUpWaves,
-                              (wave + 1) * nch / kUpWaves, a.h, a.shift, s_own[wave], out);
+    rows_product<2, kUpBurst, !FUSED>(tile, FUSED ? a.X + t * a.ldx : a.xt + (int64_t)t * a.h, used, (here + 3) >> 2,
+                                      wave * nch / kUpWaves, (wave + 1) * nch / kUpWaves, a.h, a.shift, s_own[wave], out);
     float* red = reinterpret_cast<float*>(s_own[wave]);
     wait_lds();
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) red[(r * 16 + (lane & 15)) * 17 + 4 * (lane >> 4) + i] = out[r][i];
+      for (int i = 0; i < 4; ++i) red[(r * 16 + 4 * i + (lane >> 4)) * 17 + (lane & 15)] = out[r][i];
     __syncthreads();
     if (tid < 16 * here) {
       const int c = tid >> 4, f = tid & 15;
@@ -324,18 +385,10 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs a) {
     for (int i = wave; i < n; i += kDownWaves) {
       const float* p = a.act + (int64_t)(t0 * a.k + i) * a.F;
       unsigned int m = 0u;
-      for (int f = 4 * lane; f < a.F; f += 256) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(p + f);
-        m = max(max(m, max(mag_bits(v[0]), mag_bits(v[1]))), max(mag_bits(v[2]), mag_bits(v[3])));
-      }
+      for (int f = 16 * lane; f < a.F; f += 1024) m = max(m, mag_16(p + f));
       const float s = quant8_scale(wave_umax(m));
       if (lane == 0) s_w[i] *= s;
-      for (int f = 4 * lane; f < a.F; f += 256) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(p + f);
-        float v[4] = {x[0], x[1], x[2], x[3]};
-        quant8_n(v, s);
-        *reinterpret_cast<unsigned int*>(s_qa + i * a.F + f) = pack_codes(v[0], v[1], v[2], v[3]);
-      }
+      for (int f = 16 * lane; f < a.F; f += 1024) *reinterpret_cast<u32x4*>(s_qa + i * a.F + f) = codes_16(p + f, s);
     }
   }
   __syncthreads();
@@ -353,16 +406,19 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs a) {
     }
     const Tile tile[1] = {tile_at(a.P2, a.A2, (int64_t)e * a.h + r0, a.F, a.shift)};
     for (int c0 = 0; c0 < slots; c0 += 16) {
-      const bool used = c0 + c16 < slots;
-      const int slot = used ? (int)s_col[wave][c0 + c16] : 0;
+      const bool used = c0 + slot_of_row(c16) < slots;
+      const int slot = used ? (int)s_col[wave][c0 + slot_of_row(c16)] : 0, here = min(slots - c0, 16);
       f32x4 out[1] = {{0.f, 0.f, 0.f, 0.f}};
-      rows_product<1, kDownBurst>(tile, FUSED ? s_qa + slot * a.F : a.qa + (int64_t)(t0 * a.k + slot) * a.F, used,
-                                  part * nch / parts, (part + 1) * nch / parts, a.F, a.shift, s_own[wave], out);
-      if (used) {
-        float* p = &s_sum[wave][slot / a.k][4 * (lane >> 4)];
-        const float f = s_w[slot];
+      rows_product<1, kDownBurst, true>(tile, FUSED ? s_qa + slot * a.F : a.qa + (int64_t)(t0 * a.k + slot) * a.F, used,
+                                        (here + 3) >> 2, part * nch / parts, (part + 1) * nch / parts, a.F, a.shift,
+                                        s_own[wave], out);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) p[v] = fmaf(f, out[0][v], p[v]);
+      for (int v = 0; v < 4; ++v) {
+        const int j = 4 * v + (lane >> 4);
+        if (j >= here) continue;
+        const int sl = s_col[wave][c0 + j];
+        float* p = &s_sum[wave][sl / a.k][c16];
+        *p = fmaf(s_w[sl], out[0][v], *p);
       }
     }
   }
@@ -394,7 +450,7 @@ catq_status moe_check(const catq_moe_desc* d, int64_t T) {
 }
 
 struct MoeSpace {
-  size_t ids, w, sa, hits, slots, qa, act, end;
+  size_t ids, w, sa, hits, slots, xt, qa, act, end;
 };
 MoeSpace moe_space(const catq_moe_desc* d, int64_t T) {
   const size_t n = (size_t)T * d->top_k;
@@ -404,7 +460,8 @@ MoeSpace moe_space(const catq_moe_desc* d, int64_t T) {
   s.sa = s.w + round_up(n * 4, 256);
   s.hits = s.sa + round_up(n * 4, 256);
   s.slots = s.hits + round_up((1 + 3 * (size_t)d->n_experts) * 4, 256);
-  s.qa = s.slots + round_up(n * 4, 256);
+  s.xt = s.slots + round_up(n * 4, 256);
+  s.qa = s.xt + round_up((size_t)T * d->hidden, 256);
   s.act = s.qa + round_up(n * d->ffn, 256);
   s.end = s.act + round_up(n * d->ffn * 4, 256);
   return s;
@@ -445,22 +502,27 @@ extern "C" catq_status catq_ternary_moe_a8(const catq_moe_desc* d, const float* 
   MoeArgs a{logits, q, x_scale, ldq, gu_packed, gu_alpha, down_packed, down_alpha, res, y,
             reinterpret_cast<int32_t*>(ws + sp.ids), reinterpret_cast<float*>(ws + sp.w),
             reinterpret_cast<float*>(ws + sp.act), reinterpret_cast<int8_t*>(ws + sp.qa),
-            reinterpret_cast<float*>(ws + sp.sa), reinterpret_cast<int32_t*>(ws + sp.hits),
-            reinterpret_cast<int32_t*>(ws + sp.slots), (int32_t)T, d->n_experts, d->top_k, d->hidden, d->ffn,
+            reinterpret_cast<float*>(ws + sp.sa), reinterpret_cast<int8_t*>(ws + sp.xt),
+            reinterpret_cast<int32_t*>(ws + sp.hits), reinterpret_cast<int32_t*>(ws + sp.slots), (int32_t)T, d->n_experts, d->top_k, d->hidden, d->ffn,
             __builtin_ctz((unsigned)d->group_size / 128)};
   const int n = (int)T * a.k, hit = n < a.E ? n : a.E;
   const double wt = (double)hit * a.h * a.F * (0.25 + 4.0 / d->group_size);
   const bool fused = T <= kFusedTokens, codes_here = T <= 8 && (int64_t)n * a.F <= kFusedCodes;
   if (!fused) {
     CATQ_TRACED(stream, "moe_experts_kernel", 0.0, 4.0 * T * a.E, T, a.E, a.k,
-                hipLaunchKernelGGL(moe_experts_kernel, dim3(1), dim3(1024), 0, stream, a));
+                hipLaunchKernelGGL(moe_experts_kernel, dim3(1 + (unsigned)((T * (a.h >> 4) + 1023) / 1024)), dim3(1024), 0,
+                                   stream, a));
     CATQ_CHECK_LAUNCH("moe experts");
   }
   auto up = fused ? moe_up_kernel<true> : moe_up_kernel<false>;
   CATQ_TRACED(stream, fused ? "moe_up_kernel<fused>" : "moe_up_kernel", 4.0 * n * a.h * a.F, 2.0 * wt, n, 2 * a.F, a.h,
               hipLaunchKernelGGL(up, dim3((unsigned)(a.F / 16), (unsigned)hit), dim3(kUpWaves * 64), 0, stream, a));
   CATQ_CHECK_LAUNCH("moe gate and up");
-  if (!codes_here) CATQ_TRY(catq_aux_act_quant8(a.act, CATQ_F32, n, a.F, a.F, a.qa, a.sa, stream));
+  if (!codes_here) {
+    CATQ_TRACED(stream, "moe_codes_kernel", 0.0, 5.0 * n * a.F, n, a.F, 1,
+                hipLaunchKernelGGL(moe_codes_kernel, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, stream, a));
+    CATQ_CHECK_LAUNCH("moe codes");
+  }
   const int cols = T > 16 ? 32 : 16;
   auto down = [&](auto out) {
     using Out = decltype(out);
