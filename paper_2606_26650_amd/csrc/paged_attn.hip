@@ -400,7 +400,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PaArgs a) {
       }
       const int i = row / a.G, hq = h * a.G + (row - i * a.G);
       const int64_t at = (q.row0 + i) * g.n_q + hq;
-      if (a.spans > 1) {
+      if (a.spans > 1 && !(TREE && vmax <= a.span)) {
         const int64_t pa = (int64_t)sp * g.n_tokens * g.n_q + at;
         store8<float>(a.part_o + pa * D + d8, y);
         if (d8 == 0) {
@@ -738,7 +738,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tile_kernel(PaArgs a) {
   if (odd && L != 0.f) L = __builtin_nanf("");
   const int64_t at = (q.row0 + qi) * g.n_q + hq;
   // register 4 qd + e of block d: value 32 d + 8 qd + 4 hh + e
-  if (a.spans > 1) {
+  if (a.spans > 1 && !(TREE && vmax <= a.span)) {
     const int64_t pa = (int64_t)sp * g.n_tokens * g.n_q + at;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -789,6 +789,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
   const int i = (int)(t - q.row0);
   const int r0 = (i * a.G + hq % a.G) / a.tile_rows * a.tile_rows;
   const int vmax = visible<TREE>(a, q, (min(r0 + a.tile_rows, q.n * a.G) - 1) / a.G);
+  if (TREE && vmax <= a.span) return;    // (written already)
   const int live = max((vmax + a.span - 1) / a.span, 1);
   const int64_t at = t * g.n_q + hq, step = g.n_tokens * g.n_q;
   float M = kNone;
@@ -841,6 +842,59 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PaArgs a) {
     a.lse[at] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
 }
 
+// The same for a tree, where many rows have few spans: a wave per (token, query head), D / 64 values a lane, spans in
+// order.  Rows of one span have been written already.  (Up to kWaveJoin of them; a workgroup a row takes
+// some 90 us for 1150 tokens of 40 heads, a wave 37 for 60 tokens of 8 heads and 196 spans.)
+constexpr int kWaveJoin = 16;
+template <int D>
+__global__ __launch_bounds__(256) void tree_join_kernel(PaArgs a) {
+  constexpr int N = D / 64;
+  typedef __attribute__((ext_vector_type(N))) float vec;
+  const KvGeom& g = a.g;
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= g.n_tokens * g.n_q) return;
+  const int64_t t = at / g.n_q;
+  int lo = 0, hi = g.n_seqs;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (g.cu[mid] <= t) lo = mid; else hi = mid;
+  }
+  const KvSeq q = kv_seq(g, lo);
+  if (t < q.row0 || t >= q.row0 + q.n) return;
+  const int vmax = visible<true>(a, q, 0);
+  if (vmax <= a.span) return;
+  const int live = (vmax + a.span - 1) / a.span;
+  const int64_t step = g.n_tokens * g.n_q;
+  // every lane a span's maximum and sum at a time
+  float M = kNone;
+  for (int sp = lane; sp < live; sp += 64) M = fmaxf(M, a.part_ml[2 * (sp * step + at)]);
+  M = wave_max(M);
+  float L = 0.f;
+  vec y = {};
+  for (int s0 = 0; s0 < live; s0 += 64) {
+    const int sp = s0 + lane;
+    const float w = sp < live ? exp2_fast(a.part_ml[2 * (sp * step + at)] - M) : 0.f;
+    L += sp < live ? w * a.part_ml[2 * (sp * step + at) + 1] : 0.f;
+    const int n = min(live - s0, 64);
+    const float* po = a.part_o + (s0 * step + at) * D + N * lane;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const float f = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(w), i));
+      const vec v = *reinterpret_cast<const vec*>(po + (int64_t)i * step * D);
+#pragma unroll
+      for (int j = 0; j < N; ++j) y[j] = fmaf(v[j], f, y[j]);
+    }
+  }
+  L = wave_sum(L);
+  const float inv = L > 0.f ? 1.0f / L : (L == 0.f ? 0.f : L);
+  bf16* o = a.O + at * D + N * lane;
+#pragma unroll
+  for (int j = 0; j < N; ++j) o[j] = (bf16)(y[j] * inv);
+  if (a.lse && lane == 0)
+    a.lse[at] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+}
+
 // How a call is split: rows per workgroup (16 or 32: the waves split the context; 128 or 256: the
 // waves split the rows; 256 rows share a tile's conversion, 404 us for three prompt chunks where
 // 128 take 421) and spans of the context. Both are chosen once for the batch, from max_new and
@@ -853,10 +907,14 @@ struct Plan {
   int tile_rows, row_tiles, spans, span;
 };
 
-Plan plan(const catq_kv_desc* d, const catq_kv_batch* b) {
+// A tree has tiles of 128 rows wherever it has more than 32: its rows are rarely a multiple of 256, and two workgroups to a
+// unit hide each other's barriers where no other tile shares the context (32 sequences of up to 8000 tokens, up to 60
+// drafted, 40 + 8 heads: 271 us, with 256 rows 437).  Spans of at most 2048 tokens for the longest sequences' sake
+// brought nothing (290 us, 36 of them the join), nor did loads two tiles ahead (309).
+Plan plan(const catq_kv_desc* d, const catq_kv_batch* b, bool tree) {
   const int64_t rows = (int64_t)b->max_new * (d->n_q / d->n_kv);
   Plan p;
-  p.tile_rows = rows <= 16 ? 16 : rows <= 32 || d->head_dim == 256 ? 32 : rows <= 128 ? 128 : 256;
+  p.tile_rows = rows <= 16 ? 16 : rows <= 32 || d->head_dim == 256 ? 32 : rows <= 128 || tree ? 128 : 256;
   p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
   // Spans so that the chip has 512 workgroups where the context allows (131072 tokens of one sequence:
   // 58 us; 62 with 1024, 67 with 2048), none under 256 tokens (1000 tokens of one sequence: 9.9 us; 12.4
@@ -885,14 +943,16 @@ catq_status launch_paged(const PaArgs& a, bool per_token, double flops, double b
   else if (a.tile_rows == 32) per_token ? go(paged_attn_kernel<D, 2, true, TREE>) : go(paged_attn_kernel<D, 2, false, TREE>);
   else if constexpr (D <= 128) {
     if (a.tile_rows == 128) per_token ? go(paged_tile_kernel<D, 4, true, TREE>) : go(paged_tile_kernel<D, 4, false, TREE>);
-    else per_token ? go(paged_tile_kernel<D, 8, true, TREE>) : go(paged_tile_kernel<D, 8, false, TREE>);
+    else if constexpr (!TREE) per_token ? go(paged_tile_kernel<D, 8, true, false>) : go(paged_tile_kernel<D, 8, false, false>);
   }
   CATQ_CHECK_LAUNCH("paged attention");
   if (a.spans > 1) {
-    CATQ_TRACED(stream, "paged_join_kernel", 0.0, (double)a.g.n_tokens * a.g.n_q * D * (4.0 * a.spans + 2.0),
+    const int64_t n = a.g.n_tokens * a.g.n_q;
+    const bool waves = TREE && a.spans <= kWaveJoin;
+    auto join = waves ? tree_join_kernel<D> : paged_join_kernel<D, TREE>;
+    CATQ_TRACED(stream, waves ? "tree_join_kernel" : "paged_join_kernel", 0.0, (double)n * D * (4.0 * a.spans + 2.0),
                 a.g.n_tokens, a.g.n_q, D,
-                hipLaunchKernelGGL((paged_join_kernel<D, TREE>), dim3((unsigned)(a.g.n_tokens * a.g.n_q)), dim3(256), 0,
-                                   stream, a));
+                hipLaunchKernelGGL(join, dim3((unsigned)(waves ? (n + 3) / 4 : n)), dim3(256), 0, stream, a));
     CATQ_CHECK_LAUNCH("paged attention join");
   }
   return CATQ_OK;
@@ -914,7 +974,7 @@ catq_status attend(const catq_kv_desc* d, const catq_kv_cache* cache, const catq
   CATQ_REQUIRE(aligned16(q) && aligned16(o) && aligned16(workspace) &&
                    (reinterpret_cast<uintptr_t>(lse) & 3) == 0,
                CATQ_ERR_ALIGN, "misaligned");
-  const Plan p = plan(d, batch);
+  const Plan p = plan(d, batch, tree != nullptr);
   // (a launch has fewer than 2^32 threads along x)
   CATQ_REQUIRE((int64_t)p.row_tiles * p.spans * d->n_kv < (1 << 23) &&
                    (p.spans == 1 || batch->n_tokens * d->n_q < (1 << 24)) &&
@@ -972,7 +1032,7 @@ using namespace catq;
 
 extern "C" size_t catq_paged_attention_workspace_bytes(const catq_kv_desc* d, const catq_kv_batch* b) {
   if (kv_check_sizes(d, b) != CATQ_OK || b->n_seqs == 0 || b->n_tokens == 0 || b->max_new == 0) return 0;
-  return plan_bytes(d, b, plan(d, b));
+  return std::max(plan_bytes(d, b, plan(d, b, false)), plan_bytes(d, b, plan(d, b, true)));
 }
 
 extern "C" catq_status catq_aux_paged_attention(const catq_kv_desc* d, const catq_kv_cache* cache,
