@@ -28,12 +28,13 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kT = 256;               // threads of the workgroup that picks a row's token
-constexpr int kS = 256;               // threads of one that reads a slice
+constexpr int kAloneT = 1024;         // threads of a workgroup that has a row to itself
+constexpr int kPickT = 512;           // of one that picks a row's token after others have read it
+constexpr int kS = 512;               // threads of one that reads a slice
 constexpr int kBins = 2048;
 constexpr int kList = 4096;           // composites that are gathered
 constexpr int kOne = 43;              // a weight of 1 is 2^43
-constexpr int kMaxSlices = 256;       // (kT)
+constexpr int kMaxSlices = 256;
 
 // What the workgroups of a row leave for those after them
 struct RowSpace {
@@ -114,23 +115,23 @@ __device__ __forceinline__ double least_of(float min_p) {
 __device__ __forceinline__ double exponent(const Row& r, float x) {
   return x == r.top ? 0.0 : fma((double)x, r.scale, r.offset);
 }
-__device__ __forceinline__ u64 weight(const Row& r, float x) {
-  const double z = exponent(r, x);
-  if (z < -60.0) return 0;
-  const double n = rint(z);
-  const u64 m = (u64)(unsigned int)(__builtin_amdgcn_exp2f((float)(z - n)) * 0x1p24f);
-  const int s = kOne - 24 + (int)n;      // n <= 0
-  return s >= 0 ? m << s : m >> -s;
+// 2^exponent in units of 2^-43; 0 for what is below 2^-43, -inf and NaN among it (without a branch)
+__device__ __forceinline__ u64 weight_of(double exponent) {
+  const double z = fmax(exponent, -62.0), n = rint(z);
+  const u64 m = (unsigned int)(__builtin_amdgcn_exp2f((float)(z - n)) * 0x1p24f);
+  return (m << (kOne - 24)) >> -(int)n;      // n <= 0
 }
+__device__ __forceinline__ u64 weight(const Row& r, float x) { return weight_of(exponent(r, x)); }
 // Bins of the distance from the largest logit: 64 per unit of exp's argument, the last for all that is far
 __device__ __forceinline__ int bin_of(const Row& r, float x) {
   return x == r.top ? 0 : (int)fminf((r.top - x) * r.bins, (float)(kBins - 1));
 }
 
-// f(logit, index) for the row's elements i0 .. i1 - 1, `lanes` lanes taking 16-byte pieces in turn, U loads in flight.
+// f(logit, index) for the row's elements i0 .. i1 - 1, and for those around them in the same pieces with a logit of
+// -inf, which a NaN also becomes: no branch. `lanes` lanes taking 16-byte pieces in turn, U loads in flight.
 // A row may start at any element: the pieces are aligned in memory.
 template <typename T, int U = 4, typename F>
-__device__ __forceinline__ void for_range(const T* row, int V, int i0, int i1, int lane, int lanes, F&& f) {
+__device__ __forceinline__ void for_all(const T* row, int V, int i0, int i1, int lane, int lanes, F&& f) {
   constexpr int E = 16 / sizeof(T);
   if (i0 >= i1) return;
   const int off = (int)(((uintptr_t)row & 15u) / sizeof(T));
@@ -163,12 +164,20 @@ __device__ __forceinline__ void for_range(const T* row, int V, int i0, int i1, i
         float x;
         if constexpr (sizeof(T) == 4) x = __uint_as_float(raw[0][j]);
         else x = (j & 1) ? bf16_hi(raw[0][j / 2]) : bf16_lo(raw[0][j / 2]);
-        if (x > -INFINITY && (unsigned)(i - i0) < (unsigned)(i1 - i0)) f(x, i);    // (not -inf, no NaN)
+        f(x > -INFINITY && (unsigned)(i - i0) < (unsigned)(i1 - i0) ? x : -INFINITY, i);
       }
 #pragma unroll
       for (int w = 0; w + 1 < U; ++w) raw[w] = raw[w + 1];
     }
   }
+}
+
+// f(logit, index) for the elements i0 .. i1 - 1 that can be taken: not -inf, no NaN
+template <typename T, int U = 4, typename F>
+__device__ __forceinline__ void for_range(const T* row, int V, int i0, int i1, int lane, int lanes, F&& f) {
+  for_all<T, U>(row, V, i0, i1, lane, lanes, [&](float x, int i) {
+    if (x > -INFINITY) f(x, i);
+  });
 }
 
 // v plus what another lane of the wave has, by a data-parallel move (0 where there is none)
@@ -240,12 +249,13 @@ struct Ends {
 };
 // What is gathered: all tokens up to the last bin; where they are too many, the last bin's alone; nothing where these
 // are too many too, or where top-p ends somewhere before top-k.
+// (Where top-p alone ends, tokens have not been counted: the list may turn out too short.)
 enum { kGatherAll, kGatherBin, kGatherNone };
 __device__ __forceinline__ int gathered(const Ends& e) {
   return e.count <= kList ? kGatherAll : !e.both && e.in_bin <= kList ? kGatherBin : kGatherNone;
 }
-// at: eight values in LDS
-template <int NT>
+// at: eight values in LDS.  COUNTED: the bins' tokens are counted also where there is no top-k.
+template <int NT, bool COUNTED>
 __device__ __forceinline__ Ends find_ends(const unsigned int* count, const u64* mass, int top_k, float top_p, u64* s,
                                           u64* at) {
   constexpr int B = kBins / NT;
@@ -287,10 +297,12 @@ __device__ __forceinline__ Ends find_ends(const unsigned int* count, const u64* 
   e.base = some ? at[2] : e.m_all;
   e.in_bin = some ? at[3] : 0;
   e.count = some ? at[4] : e.n_all;
+  if (!COUNTED && top_k <= 0) e.count = kList + 1;
   __syncthreads();
   return e;
 }
 
+template <int kT>
 struct Shared {
   u64 list[kList];        // what has been gathered
   u64 few[kT];            // the last tokens in question
@@ -306,14 +318,14 @@ struct Shared {
 
 // Of N sums in LDS, the one where base + their running sum passes `target` (in s.at: its index, what is before it,
 // itself).
-template <int N>
-__device__ __forceinline__ void find_passing(Shared& s, const u64* sums, u64 base, double target) {
-  constexpr int B = N / kT;
+template <int N, int kT>
+__device__ __forceinline__ void find_passing(Shared<kT>& s, const u64* sums, u64 base, double target) {
+  constexpr int B = N >= kT ? N / kT : 1;
   const int t = B * threadIdx.x;
   u64 m[B], ms = 0, all;
 #pragma unroll
   for (int i = 0; i < B; ++i) {
-    m[i] = sums[t + i];
+    m[i] = t + i < N ? sums[t + i] : 0;
     ms += m[i];
   }
   u64 em = base + block_scan<kT>(ms, s.wave, all) - ms;
@@ -345,8 +357,8 @@ struct Bound {
 // Where more than one per thread are left, the interval of composites in question is cut to one of up to 2048 parts, again
 // and again; then each thread counts the tokens ahead of its own and their weight.  (Sorting them took three times
 // as long for 100 tokens, and more for more.)
-template <typename Each>
-__device__ __forceinline__ Bound cut_bin(Shared& s, Each&& each, const Row& r, Cut q, u64 most) {
+template <int kT, typename Each>
+__device__ __forceinline__ Bound cut_bin(Shared<kT>& s, Each&& each, const Row& r, Cut q, u64 most) {
   u64 lo = 0, hi = most, before = 0;      // composites lo .. hi are in question; the weight of the bin's below lo
   const int t = threadIdx.x;
 #pragma unroll 1
@@ -449,7 +461,9 @@ __global__ __launch_bounds__(kS) void sample_first_kernel(SampleArgs a) {
   }
   if (blockIdx.x == 0 && tid == 0) sp.n = 0;
   u64 first = ~0ull;
-  for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int i) { first = min(first, composite(x, i)); });
+  for_all<T>(row, a.V, i0, i1, tid, kS, [&](float x, int i) {
+    first = min(first, x > -INFINITY ? composite(x, i) : ~0ull);
+  });
   first = block_min<kS>(first, s_wave);
   if (tid == 0) sp.first[blockIdx.x] = first;
 }
@@ -470,8 +484,9 @@ __global__ __launch_bounds__(kS) void sample_bins_kernel(SampleArgs a) {
   if (!p.filtered) {
     const double least = least_of(p.min_p);
     u64 m = 0;
-    for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) {
-      if (exponent(r, x) >= least) m += weight(r, x);
+    for_all<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) {
+      const double z = exponent(r, x);
+      m += z >= least ? weight_of(z) : 0;
     });
     m = block_sum<kS>(m, s_wave);
     if (tid == 0) sp.mass[blockIdx.x] = m;
@@ -482,16 +497,22 @@ __global__ __launch_bounds__(kS) void sample_bins_kernel(SampleArgs a) {
     s_mass[b] = 0;
   }
   __syncthreads();
-  for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) {
-    const int b = bin_of(r, x);
-    atomicAdd(&s_count[b], 1u);
-    atomicAdd(&s_mass[b], weight(r, x));
-  });
+  // numbers for top-k, weights for top-p
+  if (p.top_k <= 0) {
+    for_all<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) { atomicAdd(&s_mass[bin_of(r, x)], weight(r, x)); });
+  } else if (!(p.top_p < 1.0f)) {
+    for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) { atomicAdd(&s_count[bin_of(r, x)], 1u); });
+  } else {
+    for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int) {
+      const int b = bin_of(r, x);
+      atomicAdd(&s_count[b], 1u);
+      atomicAdd(&s_mass[b], weight(r, x));
+    });
+  }
   __syncthreads();
   for (int b = tid; b < kBins; b += kS) {
-    if (!s_count[b]) continue;
-    atomicAdd(&sp.bin_count[b], s_count[b]);
-    atomicAdd(&sp.bin_mass[b], s_mass[b]);
+    if (s_count[b]) atomicAdd(&sp.bin_count[b], s_count[b]);
+    if (s_mass[b]) atomicAdd(&sp.bin_mass[b], s_mass[b]);
   }
 }
 
@@ -510,7 +531,7 @@ __global__ __launch_bounds__(kS) void sample_gather_kernel(SampleArgs a) {
   const u64 first = block_min<kS>(tid < a.slices ? sp.first[tid] : ~0ull, s_wave);
   if (first == ~0ull) return;
   const Row r = row_of(first, p.temp);
-  const Ends e = find_ends<kS>(sp.bin_count, sp.bin_mass, p.top_k, p.top_p, s_wave, s_at);
+  const Ends e = find_ends<kS, false>(sp.bin_count, sp.bin_mass, p.top_k, p.top_p, s_wave, s_at);
   const int what = gathered(e);
   if (what == kGatherNone) return;
   if (tid == 0) s_n = 0;
@@ -526,10 +547,11 @@ __global__ __launch_bounds__(kS) void sample_gather_kernel(SampleArgs a) {
       if (bin_of(r, x) <= e.last) add(x, i);
     });
   } else {
-    for_range<T>(row, a.V, i0, i1, tid, kS, [&](float x, int i) {
+    for_all<T>(row, a.V, i0, i1, tid, kS, [&](float x, int i) {
       const int b = bin_of(r, x);
-      if (b < e.last && exponent(r, x) >= least) m += weight(r, x);
-      if (b == e.last) add(x, i);
+      const double z = exponent(r, x);
+      m += b < e.last && z >= least ? weight_of(z) : 0;
+      if (b == e.last && x > -INFINITY) add(x, i);
     });
     m = block_sum<kS>(m, s_wave);
     if (tid == 0) sp.mass[blockIdx.x] = m;
@@ -546,8 +568,9 @@ __global__ __launch_bounds__(kS) void sample_gather_kernel(SampleArgs a) {
 
 // SLICED: with what the kernels above have left; otherwise from the row alone.
 template <typename T, bool SLICED>
-__global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
-  __shared__ Shared s;
+__global__ __launch_bounds__(SLICED ? kPickT : kAloneT) void sample_kernel(SampleArgs a) {
+  constexpr int kT = SLICED ? kPickT : kAloneT;
+  __shared__ Shared<kT> s;
   const int64_t r0 = blockIdx.x;
   const T* row = static_cast<const T*>(a.logits) + r0 * a.ld;
   const int tid = threadIdx.x, V = a.V;
@@ -588,10 +611,16 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
       });
       __syncthreads();
     }
-    const Ends e = find_ends<kT>(s.count, s.mass, p.top_k, p.top_p, s.wave, s.at);
+    const Ends e = find_ends<kT, !SLICED>(s.count, s.mass, p.top_k, p.top_p, s.wave, s.at);
     what = gathered(e);
+    unsigned int in_bin = (unsigned int)e.in_bin;
     if constexpr (SLICED) {
-      if (what != kGatherNone) n = (int)(what == kGatherAll ? e.count : e.in_bin);
+      if (what != kGatherNone) {
+        const unsigned int have = sp->n;
+        if (what == kGatherBin) in_bin = have;
+        if (have > kList) what = kGatherNone;
+        n = what == kGatherNone ? 0 : (int)have;
+      }
       for (int i = tid; i < n; i += kT) s.list[i] = sp->list[i];
     } else if (what == kGatherAll) {
       n = (int)e.count;
@@ -607,7 +636,7 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
     }
     __syncthreads();
     u64 sum = e.m_all;          // the weight that top-k keeps
-    Cut q = {e.last, (int)e.in_bin, false, e.want, e.base, 0.0};
+    Cut q = {e.last, (int)in_bin, false, e.want, e.base, 0.0};
 #pragma unroll 1
     for (int filter = e.by_k ? 0 : 1; filter < (p.top_p < 1.0f ? 2 : 1); ++filter) {
       if (filter == 1) {
@@ -632,7 +661,7 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
         __syncthreads();
         q.bin = (int)s.at[0];
         q.base = s.at[2];
-        q.n = (int)s.at[3];
+        q.n = SLICED && p.top_k <= 0 ? (int)in_bin : (int)s.at[3];
         __syncthreads();
       }
       const Bound end = cut_bin(s, [&](auto&& f) __attribute__((always_inline)) {
@@ -646,7 +675,6 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
       sum = q.base + end.mass;
     }
   }
-  auto kept = [&](float x, int i) { return composite(x, i) <= bound && exponent(r, x) >= least; };
   if (what == kGatherAll) {
     // all that is kept is in the list: its weight by 1024 parts of the vocabulary, then within the part where u falls
     u64 m[kList / kT], all = 0;
@@ -718,8 +746,9 @@ __global__ __launch_bounds__(kT) void sample_kernel(SampleArgs a) {
   for (;; whole = false) {
     const int len = (i1 - i0 + kT - 1) / kT, a0 = min(i0 + tid * len, i1), a1 = min(a0 + len, i1);
     u64 m = 0;
-    for_range<T>(row, V, a0, a1, 0, 1, [&](float x, int i) {
-      if (kept(x, i)) m += weight(r, x);
+    for_all<T>(row, V, a0, a1, 0, 1, [&](float x, int i) {
+      const double z = exponent(r, x);
+      m += composite(x, i) <= bound && z >= least ? weight_of(z) : 0;      // (-inf weighs nothing)
     });
     if (whole) {
       all = (double)block_sum<kT>(m, s.wave);
@@ -758,7 +787,7 @@ catq_status launch_sample(SampleArgs a, int64_t rows, hipStream_t stream) {
   const double bytes = (double)rows * a.V * sizeof(T);
   if (a.V <= kAlone) {
     CATQ_TRACED(stream, "sample_kernel<alone>", 0.0, bytes, rows, a.V, 1,
-                hipLaunchKernelGGL((sample_kernel<T, false>), dim3((unsigned)rows), dim3(kT), 0, stream, a));
+                hipLaunchKernelGGL((sample_kernel<T, false>), dim3((unsigned)rows), dim3(kAloneT), 0, stream, a));
     CATQ_CHECK_LAUNCH("sample");
     return CATQ_OK;
   }
@@ -774,7 +803,7 @@ catq_status launch_sample(SampleArgs a, int64_t rows, hipStream_t stream) {
     CATQ_TRACED(stream, "sample_gather_kernel", 0.0, bytes, rows, a.V, sl.n,
                 hipLaunchKernelGGL((sample_gather_kernel<T>), grid, dim3(kS), 0, stream, a));
   CATQ_TRACED(stream, "sample_kernel", 0.0, 0.0, rows, a.V, 1,
-              hipLaunchKernelGGL((sample_kernel<T, true>), dim3((unsigned)rows), dim3(kT), 0, stream, a));
+              hipLaunchKernelGGL((sample_kernel<T, true>), dim3((unsigned)rows), dim3(kPickT), 0, stream, a));
   CATQ_CHECK_LAUNCH("sample");
   return CATQ_OK;
 }
