@@ -8,9 +8,9 @@
 // into LDS of its own at once by direct copies, so that a unit has some 100 KB in flight without a wait between waves;
 // the matrix products take 16 slots, of which a few are used.
 //
-// Launches.  Up to four tokens: every workgroup of the first kernel finds the tokens' experts itself, and where the
-// codes of a are few every workgroup of the second forms them itself: two launches. More tokens: the experts and
-// their slots are laid out by a kernel of their own, and so are the codes.
+// Launches.  One token: every wave of the first kernel finds its experts itself, every workgroup of the second forms the
+// codes of a: two launches.  More tokens: the experts and their slots are laid out by a kernel of their own (in the first
+// kernel, two tokens took as long, four 54 us instead of 49.5), and so are the codes where they are more than LDS takes.
 #include <type_traits>
 
 #include "kernels.h"
@@ -71,6 +71,21 @@ constexpr int own_bytes() {
 // element of every lane is converted and scaled.
 __device__ __forceinline__ int slot_of_row(int row) { return 4 * (row & 3) + (row >> 2); }
 
+// The copies of nb <= NB chunks' codes from chunk b0 on into a wave's LDS.
+template <int R, int NB>
+__device__ __forceinline__ void copy_codes(const Tile (&tile)[R], int b0, int nb, int n, char* own) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)own;
+  const uint32_t woff = (uint32_t)((lane >> 2) * (n >> 2) + ((lane & 3) ^ (lane >> 4)) * 16);
+#pragma unroll
+  for (int p = 0; p < NB / 2; ++p) {
+    if (2 * p >= nb) continue;
+#pragma unroll
+    for (int r = 0; r < R; ++r)    // (past a row's end: the next row, or zeros; never used)
+      dma16_lds(tile[r].codes, woff + (uint32_t)(b0 + 2 * p) * 32u, 0u, lds + (r * (NB / 2) + p) * 1024);
+  }
+}
+
 // out[r][e] += sum over chunks c0 .. c1 - 1 of alpha * (codes . x) of weight row lane % 16 of tile r and slot
 // 4 e + lane / 16, e < ne. x: the activations of this lane's row, if it has a slot. n: codes of a row. NB chunks at a
 // time. ORDERED: the activations are in the order of the operands.
@@ -79,20 +94,12 @@ __device__ __forceinline__ void rows_product(const Tile (&tile)[R], const int8_t
                                              int n, int shift, char* own, f32x4 (&out)[R]) {
   constexpr int G = scale_slots(NB), AU = 16 * G / 64;
   const int lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
-  const int row_bytes = n >> 2, ng = n >> (7 + shift);
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)own;
+  const int ng = n >> (7 + shift);
   float* s_al = reinterpret_cast<float*>(own + R * (NB / 2 * 1024));
-  const uint32_t woff = (uint32_t)((lane >> 2) * row_bytes + ((lane & 3) ^ (lane >> 4)) * 16);
   for (int b0 = c0; b0 < c1; b0 += NB) {
     const int nb = min(c1 - b0, NB), g0 = b0 >> shift;
     wait_lds();     // what the last burst read may be written over
-#pragma unroll
-    for (int p = 0; p < NB / 2; ++p) {
-      if (2 * p >= nb) continue;
-#pragma unroll
-      for (int r = 0; r < R; ++r)    // (past a row's end: the next row, or zeros; never used)
-        dma16_lds(tile[r].codes, woff + (uint32_t)(b0 + 2 * p) * 32u, 0u, lds + (r * (NB / 2) + p) * 1024);
-    }
+    copy_codes<R, NB>(tile, b0, nb, n, own);
     float av[R][AU];
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -258,15 +265,13 @@ __global__ __launch_bounds__(256) void moe_codes_kernel(MoeArgs a) {
 }
 
 // Gate, up and their product: 16 values of a for all slots of an expert.
-// FUSED (a token per wave): the workgroup finds the tokens' experts; item i is the expert of slot i, if none before it
-// has the same, or, where there are more slots than experts, expert i if any slot has it. Otherwise item i is the
-// i-th expert that is hit.
-constexpr int kUpWaves = 4, kUpBurst = 8, kFusedTokens = kUpWaves;
+// FUSED (one token): every wave finds the token's experts, item i is that of slot i. Otherwise item i is the i-th expert
+// that is hit.
+constexpr int kUpWaves = 4, kUpBurst = 8;
 template <bool FUSED>
 __global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
   constexpr int OWN = own_bytes<2, kUpBurst>();
   __shared__ __align__(16) char s_own[kUpWaves][OWN];
-  __shared__ int s_ids[FUSED ? kFusedTokens * 16 : 1];
   __shared__ int s_slot[16];
   static_assert(OWN >= 2 * 16 * 17 * 4, "the waves' sums fit their place");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -274,32 +279,15 @@ __global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
   int e, slots;
   const int32_t* list = nullptr;
   if constexpr (FUSED) {
-    const int n = a.T * a.k;
-    for (int t = wave; t < a.T; t += kUpWaves) {
-      int id;
-      float w;
-      topk_any(a, t, lane, id, w);
-      if (lane < a.k) {
-        s_ids[t * a.k + lane] = id;
-        if (blockIdx.x == 0 && item == 0) {
-          a.ids[t * a.k + lane] = id;
-          a.w[t * a.k + lane] = w;
-        }
-      }
+    int id;
+    float w;
+    topk_any(a, 0, lane, id, w);
+    if (blockIdx.x == 0 && item == 0 && tid < a.k) {
+      a.ids[tid] = id;
+      a.w[tid] = w;
     }
-    __syncthreads();
-    e = __builtin_amdgcn_readfirstlane(n <= a.E ? s_ids[item] : item);
-    slots = 0;
-    bool first = true;
-    for (int b = 0; b < n; b += 64) {      // (an expert is hit once by a token)
-      const bool mine = b + lane < n && s_ids[b + lane] == e;
-      const unsigned long long m = __ballot(mine);
-      if (n <= a.E && slots == 0 && m && b + __builtin_ctzll(m) < item) first = false;
-      if (wave == 0 && mine) s_slot[slots + __popcll(m & ((1ull << lane) - 1))] = b + lane;
-      slots += __popcll(m);
-    }
-    if (!first || slots == 0) return;
-    __syncthreads();
+    e = __builtin_amdgcn_readlane(id, item);
+    slots = 1;
   } else {
     if (item >= a.hits[0]) return;
     const int32_t* h = a.hits + 1 + 3 * item;
@@ -312,9 +300,9 @@ __global__ __launch_bounds__(kUpWaves * 64) void moe_up_kernel(MoeArgs a) {
   const Tile tile[2] = {tile_at(a.P1, a.A1, row, a.h, a.shift), tile_at(a.P1, a.A1, row + a.F, a.h, a.shift)};
   for (int s0 = 0; s0 < slots; s0 += 16) {
     const int here = min(slots - s0, 16), mine = slot_of_row(lane & 15);
-    if (!FUSED && tid < here) s_slot[tid] = list[s0 + tid];
+    if (tid < here) s_slot[tid] = FUSED ? item : list[s0 + tid];
     const bool used = mine < here;
-    const int slot = !used ? 0 : FUSED ? s_slot[mine] : list[s0 + mine];
+    const int slot = !used ? 0 : FUSED ? item : list[s0 + mine];
     const int t = slot / a.k;
     f32x4 out[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     rows_product<2, kUpBurst, !FUSED>(tile, FUSED ? a.X + t * a.ldx : a.xt + (int64_t)t * a.h, used, (here + 3) >> 2,
@@ -381,6 +369,10 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs a) {
       s_list[at] = (short)tid;
     }
   }
+  __syncthreads();
+  const int r0 = blockIdx.x * 16, c16 = lane & 15, nch = a.F >> 7;
+  int parts = 1;
+  while (hit * parts < kDownWaves && 2 * parts <= nch) parts *= 2;
   if constexpr (FUSED) {
     for (int i = wave; i < n; i += kDownWaves) {
       const float* p = a.act + (int64_t)(t0 * a.k + i) * a.F;
@@ -390,11 +382,8 @@ __global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(MoeArgs a) {
       if (lane == 0) s_w[i] *= s;
       for (int f = 16 * lane; f < a.F; f += 1024) *reinterpret_cast<u32x4*>(s_qa + i * a.F + f) = codes_16(p + f, s);
     }
+    __syncthreads();
   }
-  __syncthreads();
-  const int r0 = blockIdx.x * 16, c16 = lane & 15, nch = a.F >> 7;
-  int parts = 1;
-  while (hit * parts < kDownWaves && 2 * parts <= nch) parts *= 2;
   for (int i = wave; i < hit * parts; i += kDownWaves) {
     const int e = __builtin_amdgcn_readfirstlane((int)s_list[i / parts]), part = i % parts;
     int slots = 0;
@@ -507,7 +496,7 @@ extern "C" catq_status catq_ternary_moe_a8(const catq_moe_desc* d, const float* 
             __builtin_ctz((unsigned)d->group_size / 128)};
   const int n = (int)T * a.k, hit = n < a.E ? n : a.E;
   const double wt = (double)hit * a.h * a.F * (0.25 + 4.0 / d->group_size);
-  const bool fused = T <= kFusedTokens, codes_here = T <= 8 && (int64_t)n * a.F <= kFusedCodes;
+  const bool fused = T == 1, codes_here = T <= 8 && (int64_t)n * a.F <= kFusedCodes;
   if (!fused) {
     CATQ_TRACED(stream, "moe_experts_kernel", 0.0, 4.0 * T * a.E, T, a.E, a.k,
                 hipLaunchKernelGGL(moe_experts_kernel, dim3(1 + (unsigned)((T * (a.h >> 4) + 1023) / 1024)), dim3(1024), 0,
