@@ -443,7 +443,7 @@ def catq_ternary_moe_a8_workspace_bytes(desc, T):
     return int(lib.catq_ternary_moe_a8_workspace_bytes(C.byref(desc), T))
 
 
-def catq_ternary_moe_a8(desc, logits, q, x_scale, gu_packed, gu_alpha, down_packed, down_alpha, y, workspace,
+def catq_ternary_moe_a8(desc, logits, q, x_scale, gu_packed, gu_alpha, down_packed, down_alpha, y, workspace=None,
                         res=None, stream=None):
     """y = res + the routed experts' output of few tokens: logits fp32 [T][E], codes q int8 [T][hidden] (rows may be
     strided) with x_scale fp32 [T], gu_packed uint8 [E][2 ffn][hidden/4], down_packed uint8 [E][hidden][ffn/4] and
@@ -463,11 +463,11 @@ def catq_ternary_moe_a8(desc, logits, q, x_scale, gu_packed, gu_alpha, down_pack
     _want(y, "y", y.dtype, (T, h), dev)
     if res is not None:
         _want(res, "res", y.dtype, (T, h), dev)
-    if workspace.get_device() != dev or not workspace.is_contiguous():
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError(f"workspace: must be contiguous and on GPU {dev}")
     _run_on(dev, stream, lib.catq_ternary_moe_a8, "catq_ternary_moe_a8", C.byref(d), logits.data_ptr(), q.data_ptr(), T,
             ldq, x_scale.data_ptr(), gu_packed.data_ptr(), gu_alpha.data_ptr(), down_packed.data_ptr(),
-            down_alpha.data_ptr(), _ptr(res), y.data_ptr(), yd, workspace.data_ptr(), _bytes(workspace))
+            down_alpha.data_ptr(), _ptr(res), y.data_ptr(), yd, _ptr(workspace), _bytes(workspace))
 
 
 def _int32(**sizes):

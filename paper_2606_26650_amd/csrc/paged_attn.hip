@@ -878,7 +878,6 @@ __global__ __launch_bounds__(256) void tree_join_kernel(PaArgs a) {
     L += sp < live ? w * a.part_ml[2 * (sp * step + at) + 1] : 0.f;
     const int n = min(live - s0, 64);
     const float* po = a.part_o + (s0 * step + at) * D + N * lane;
-#pragma unroll 4
     for (int i = 0; i < n; ++i) {
       const float f = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(w), i));
       const vec v = *reinterpret_cast<const vec*>(po + (int64_t)i * step * D);

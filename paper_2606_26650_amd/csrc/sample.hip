@@ -462,7 +462,8 @@ __global__ __launch_bounds__(kS) void sample_first_kernel(SampleArgs a) {
   if (blockIdx.x == 0 && tid == 0) sp.n = 0;
   u64 first = ~0ull;
   for_all<T>(row, a.V, i0, i1, tid, kS, [&](float x, int i) {
-    first = min(first, x > -INFINITY ? composite(x, i) : ~0ull);
+    const u64 c = composite(x, i);
+    first = x > -INFINITY && c < first ? c : first;
   });
   first = block_min<kS>(first, s_wave);
   if (tid == 0) sp.first[blockIdx.x] = first;

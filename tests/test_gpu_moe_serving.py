@@ -110,7 +110,9 @@ CASES = [
     (3, 16, 3, 1152, 256, 128), (5, 60, 6, 256, 1408, 128), (7, 8, 1, 512, 512, 256), (16, 8, 2, 256, 256, 128),
     (17, 6, 5, 384, 128, 128), (33, 128, 8, 256, 256, 128), (40, 3, 2, 1024, 1024, 512), (64, 5, 1, 128, 384, 128),
     (130, 12, 4, 256, 128, 128), (1, 1024, 16, 128, 128, 128), (20, 300, 16, 128, 256, 128), (4, 2, 2, 2304, 128, 128),
-    (2, 3, 2, 4096, 2176, 128), (9, 4, 2, 2048, 1024, 1024),
+    (2, 3, 2, 4096, 2176, 128), (9, 4, 2, 2048, 1024, 1024), (1, 4, 4, 256, 8192, 128), (8, 6, 4, 256, 256, 128),
+    (1, 6, 2, 1024, 512, 256), (300, 20, 16, 128, 128, 128), (1024, 4, 1, 128, 128, 128), (1, 1, 1, 32768, 128, 128),
+    (2, 2, 1, 128, 32768, 128), (32, 40, 2, 384, 1664, 128),
 ]
 
 
