@@ -128,54 +128,43 @@ __device__ __forceinline__ int bin_of(const Row& r, float x) {
 }
 
 // f(logit, index) for the row's elements i0 .. i1 - 1, and for those around them in the same pieces with a logit of
-// -inf, which a NaN also becomes: no branch. `lanes` lanes taking 16-byte pieces in turn, U loads in flight.
-// A row may start at any element: the pieces are aligned in memory.
-template <typename T, int U = 4, typename F>
+// -inf, which a NaN also becomes: no branch. `lanes` lanes take 16-byte pieces in turn. A row may start at any
+// element: the pieces are aligned in memory. (Several pieces in flight a lane, moved up as they are used, took 3 to 10%
+// longer: the waves of a unit hide each other's loads.)
+template <typename T, typename F>
 __device__ __forceinline__ void for_all(const T* row, int V, int i0, int i1, int lane, int lanes, F&& f) {
   constexpr int E = 16 / sizeof(T);
   if (i0 >= i1) return;
   const int off = (int)(((uintptr_t)row & 15u) / sizeof(T));
   const int v1 = (i1 - 1 + off) / E;
-  for (int v = (i0 + off) / E + lane; v <= v1; v += U * lanes) {
-    u32x4 raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int e0 = (v + u * lanes) * E - off;
-      if (v + u * lanes > v1) continue;
-      if (e0 >= 0 && e0 + E <= V) {
-        raw[u] = *reinterpret_cast<const u32x4*>(row + e0);
-      } else {                         // the first or last piece of the row
-        raw[u] = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          if (e0 + j < 0 || e0 + j >= V) continue;
-          if constexpr (sizeof(T) == 4) raw[u][j] = __builtin_bit_cast(unsigned int, row[e0 + j]);
-          else raw[u][j / 2] |= (unsigned)__builtin_bit_cast(u16, row[e0 + j]) << (16 * (j & 1));
-        }
-      }
-    }
-    // one piece at a time, the others moved up: the code is there once
-#pragma unroll 1
-    for (int u = 0; u < U && v + u * lanes <= v1; ++u) {
-      const int e0 = (v + u * lanes) * E - off;
+  for (int v = (i0 + off) / E + lane; v <= v1; v += lanes) {
+    const int e0 = v * E - off;
+    u32x4 raw = {0u, 0u, 0u, 0u};
+    if (e0 >= 0 && e0 + E <= V) {
+      raw = *reinterpret_cast<const u32x4*>(row + e0);
+    } else {                         // the first or last piece of the row
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        const int i = e0 + j;
-        float x;
-        if constexpr (sizeof(T) == 4) x = __uint_as_float(raw[0][j]);
-        else x = (j & 1) ? bf16_hi(raw[0][j / 2]) : bf16_lo(raw[0][j / 2]);
-        f(x > -INFINITY && (unsigned)(i - i0) < (unsigned)(i1 - i0) ? x : -INFINITY, i);
+        if (e0 + j < 0 || e0 + j >= V) continue;
+        if constexpr (sizeof(T) == 4) raw[j] = __builtin_bit_cast(unsigned int, row[e0 + j]);
+        else raw[j / 2] |= (unsigned)__builtin_bit_cast(u16, row[e0 + j]) << (16 * (j & 1));
       }
+    }
 #pragma unroll
-      for (int w = 0; w + 1 < U; ++w) raw[w] = raw[w + 1];
+    for (int j = 0; j < E; ++j) {
+      const int i = e0 + j;
+      float x;
+      if constexpr (sizeof(T) == 4) x = __uint_as_float(raw[j]);
+      else x = (j & 1) ? bf16_hi(raw[j / 2]) : bf16_lo(raw[j / 2]);
+      f(x > -INFINITY && (unsigned)(i - i0) < (unsigned)(i1 - i0) ? x : -INFINITY, i);
     }
   }
 }
 
 // f(logit, index) for the elements i0 .. i1 - 1 that can be taken: not -inf, no NaN
-template <typename T, int U = 4, typename F>
+template <typename T, typename F>
 __device__ __forceinline__ void for_range(const T* row, int V, int i0, int i1, int lane, int lanes, F&& f) {
-  for_all<T, U>(row, V, i0, i1, lane, lanes, [&](float x, int i) {
+  for_all<T>(row, V, i0, i1, lane, lanes, [&](float x, int i) {
     if (x > -INFINITY) f(x, i);
   });
 }
