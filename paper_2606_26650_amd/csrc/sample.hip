@@ -33,6 +33,7 @@ constexpr int kPickT = 512;           // of one that picks a row's token after o
 constexpr int kS = 512;               // threads of one that reads a slice
 constexpr int kBins = 2048;
 constexpr int kList = 4096;           // composites that are gathered
+constexpr int kFew = 128;             // that are compared with each other, if they are at hand
 constexpr int kOne = 43;              // a weight of 1 is 2^43
 constexpr int kMaxSlices = 256;
 
@@ -131,36 +132,39 @@ __device__ __forceinline__ int bin_of(const Row& r, float x) {
 // -inf, which a NaN also becomes: no branch. `lanes` lanes take 16-byte pieces in turn. A row may start at any
 // element: the pieces are aligned in memory. (Several pieces in flight a lane, moved up as they are used, took 3 to 10%
 // longer: the waves of a unit hide each other's loads.)
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece(const T* row, int V, int e0) {
+  constexpr int E = 16 / sizeof(T);
+  if (e0 >= 0 && e0 + E <= V) return *reinterpret_cast<const u32x4*>(row + e0);
+  u32x4 raw = {0u, 0u, 0u, 0u};      // the first or last piece of the row
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    if (e0 + j < 0 || e0 + j >= V) continue;
+    if constexpr (sizeof(T) == 4) raw[j] = __builtin_bit_cast(unsigned int, row[e0 + j]);
+    else raw[j / 2] |= (unsigned)__builtin_bit_cast(u16, row[e0 + j]) << (16 * (j & 1));
+  }
+  return raw;
+}
+template <typename T, typename F>
+__device__ __forceinline__ void use_piece(u32x4 raw, int e0, int i0, int i1, F&& f) {
+#pragma unroll
+  for (int j = 0; j < (int)(16 / sizeof(T)); ++j) {
+    const int i = e0 + j;
+    float x;
+    if constexpr (sizeof(T) == 4) x = __uint_as_float(raw[j]);
+    else x = (j & 1) ? bf16_hi(raw[j / 2]) : bf16_lo(raw[j / 2]);
+    f(x > -INFINITY && (unsigned)(i - i0) < (unsigned)(i1 - i0) ? x : -INFINITY, i);
+  }
+}
 template <typename T, typename F>
 __device__ __forceinline__ void for_all(const T* row, int V, int i0, int i1, int lane, int lanes, F&& f) {
   constexpr int E = 16 / sizeof(T);
   if (i0 >= i1) return;
   const int off = (int)(((uintptr_t)row & 15u) / sizeof(T));
   const int v1 = (i1 - 1 + off) / E;
-  for (int v = (i0 + off) / E + lane; v <= v1; v += lanes) {
-    const int e0 = v * E - off;
-    u32x4 raw = {0u, 0u, 0u, 0u};
-    if (e0 >= 0 && e0 + E <= V) {
-      raw = *reinterpret_cast<const u32x4*>(row + e0);
-    } else {                         // the first or last piece of the row
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        if (e0 + j < 0 || e0 + j >= V) continue;
-        if constexpr (sizeof(T) == 4) raw[j] = __builtin_bit_cast(unsigned int, row[e0 + j]);
-        else raw[j / 2] |= (unsigned)__builtin_bit_cast(u16, row[e0 + j]) << (16 * (j & 1));
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-      const int i = e0 + j;
-      float x;
-      if constexpr (sizeof(T) == 4) x = __uint_as_float(raw[j]);
-      else x = (j & 1) ? bf16_hi(raw[j / 2]) : bf16_lo(raw[j / 2]);
-      f(x > -INFINITY && (unsigned)(i - i0) < (unsigned)(i1 - i0) ? x : -INFINITY, i);
-    }
-  }
+  for (int v = (i0 + off) / E + lane; v <= v1; v += lanes)
+    use_piece<T>(load_piece(row, V, v * E - off), v * E - off, i0, i1, f);
 }
-
 // f(logit, index) for the elements i0 .. i1 - 1 that can be taken: not -inf, no NaN
 template <typename T, typename F>
 __device__ __forceinline__ void for_range(const T* row, int V, int i0, int i1, int lane, int lanes, F&& f) {
@@ -343,15 +347,16 @@ struct Bound {
 };
 
 // each(f) calls f(logit, composite) for all tokens of the row that may be in the bin; those with c <= most count.
-// Where more than one per thread are left, the interval of composites in question is cut to one of up to 2048 parts, again
-// and again; then each thread counts the tokens ahead of its own and their weight.  (Sorting them took three times
-// as long for 100 tokens, and more for more.)
+// Where more than `few` (at most kT) are left, the interval of composites in question is cut to one of up to 2048 parts, again
+// and again; then a thread for each counts the tokens ahead of its own and their weight.  (Sorting 100 of them took three
+// times as long; counting among 500 took 20 us.)
 template <int kT, typename Each>
-__device__ __forceinline__ Bound cut_bin(Shared<kT>& s, Each&& each, const Row& r, Cut q, u64 most) {
+__device__ __forceinline__ Bound cut_bin(Shared<kT>& s, Each&& each, const Row& r, Cut q, u64 most,
+                                         int few) {
   u64 lo = 0, hi = most, before = 0;      // composites lo .. hi are in question; the weight of the bin's below lo
   const int t = threadIdx.x;
 #pragma unroll 1
-  while (q.n > kT) {
+  while (q.n > few) {
     u64 least = ~0ull, last = 0;
     each([&](float x, u64 c) {
       if (bin_of(r, x) != q.bin || c < lo || c > hi) return;
@@ -413,20 +418,22 @@ __device__ __forceinline__ Bound cut_bin(Shared<kT>& s, Each&& each, const Row& 
   __syncthreads();
   const int n = (int)min(s.n, (unsigned)kT);
   const u64 c = t < n ? s.few[t] : 0, m = t < n ? weight(r, logit_of(c)) : 0;
-  s.weight[t] = m;
+  if (t < n) s.weight[t] = m;
   __syncthreads();
-  u64 em = before, rank = 0;
+  if (t < n) {
+    u64 em = before, rank = 0;
 #pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const bool ahead = s.few[i] < c;
-    rank += ahead ? 1 : 0;
-    em += ahead ? s.weight[i] : 0;
-  }
-  const bool here = q.by_mass ? (double)(q.base + em) < q.target && q.target <= (double)(q.base + em + m)
-                              : rank + 1 == q.want;
-  if (t < n && here) {
-    s.at[0] = c;
-    s.at[1] = em + m;
+    for (int i = 0; i < n; ++i) {
+      const bool ahead = s.few[i] < c;
+      rank += ahead ? 1 : 0;
+      em += ahead ? s.weight[i] : 0;
+    }
+    const bool here = q.by_mass ? (double)(q.base + em) < q.target && q.target <= (double)(q.base + em + m)
+                                : rank + 1 == q.want;
+    if (here) {
+      s.at[0] = c;
+      s.at[1] = em + m;
+    }
   }
   __syncthreads();
   const Bound out = {s.at[0], s.at[1]};
@@ -660,7 +667,7 @@ __global__ __launch_bounds__(SLICED ? kPickT : kAloneT) void sample_kernel(Sampl
         } else {
           for_range<T>(row, V, 0, V, tid, kT, [&](float x, int i) { f(x, composite(x, i)); });
         }
-      }, r, q, bound);
+      }, r, q, bound, what != kGatherNone ? kFew : kT);
       bound = min(bound, end.c);
       sum = q.base + end.mass;
     }
