@@ -16,7 +16,7 @@
 // by slices of the row, of which the one where u falls is read again.  Only in the bins in which a filter ends are tokens compared.
 // Without top-k and top-p no bins are needed, only the weight of every slice.
 //
-// Rows of more than kAlone tokens are read by several workgroups each: the largest logit of every slice, then bins
+// Long rows are read by several workgroups each: the largest logit of every slice, then bins
 // or weights of every slice, then the gathering, then one workgroup a row for what is left.
 //
 // What bounds it: for few rows the launches, 11 us for four, and the chains of latencies in them (150000 fp32 logits: greedy 12 us,
@@ -40,6 +40,7 @@ constexpr int kBins = 2048;
 constexpr int kList = 4096;           // composites that are gathered
 constexpr int kFew = 128;             // that are compared with each other, if they are at hand
 constexpr int kOne = 43;              // a weight of 1 is 2^43
+constexpr int kWide = 32;             // tokens that a thread reads in a row at most
 constexpr int kMaxSlices = 256;
 
 // What the workgroups of a row leave for those after them
@@ -744,11 +745,9 @@ __global__ __launch_bounds__(SLICED ? kPickT : kAloneT) void sample_kernel(Sampl
     base = s.at[1];
     whole = false;
   }
-#pragma unroll 1
-  for (;; whole = false) {
-    const int len = (i1 - i0 + kT - 1) / kT, a0 = min(i0 + tid * len, i1), a1 = min(a0 + len, i1);
+  auto weigh = [&](int a0, int a1, int lane, int lanes) __attribute__((always_inline)) {
     u64 m = 0;
-    for_all<T>(row, V, a0, a1, 0, 1, [&](float x, int i) {
+    for_all<T>(row, V, a0, a1, lane, lanes, [&](float x, int i) {
       const double z = exponent(r, x);
       m += composite(x, i) <= bound && z >= least ? weight_of(z) : 0;      // (-inf weighs nothing)
     });
@@ -756,13 +755,33 @@ __global__ __launch_bounds__(SLICED ? kPickT : kAloneT) void sample_kernel(Sampl
       all = (double)block_sum<kT>(m, s.wave);
       target = (double)u * all;
     }
+    return m;
+  };
+  auto take = [&](int len) __attribute__((always_inline)) {
+    i0 = min(i0 + (int)s.at[0] * len, i1);
+    i1 = min(i0 + len, i1);
+    base = s.at[1];
+  };
+  constexpr int W = kT / 64;
+#pragma unroll 1
+  for (; i1 - i0 > kWide * kT; whole = false) {      // (long parts by waves, whose loads are consecutive)
+    const int len = (i1 - i0 + W - 1) / W, a0 = min(i0 + (tid >> 6) * len, i1);
+    const u64 m = wave_scan(weigh(a0, min(a0 + len, i1), tid & 63, 64));
+    __syncthreads();
+    if ((tid & 63) == 63) s.mass[tid >> 6] = m;
+    __syncthreads();
+    find_passing<W>(s, s.mass, base, target);
+    take(len);
+  }
+#pragma unroll 1
+  for (;; whole = false) {
+    const int len = (i1 - i0 + kT - 1) / kT, a0 = min(i0 + tid * len, i1);
+    const u64 m = weigh(a0, min(a0 + len, i1), 0, 1);
     __syncthreads();
     s.mass[tid] = m;
     __syncthreads();
     find_passing<kT>(s, s.mass, base, target);
-    i0 = min(i0 + (int)s.at[0] * len, i1);
-    i1 = min(i0 + len, i1);
-    base = s.at[1];
+    take(len);
     if (len == 1) break;
   }
   if (tid == 0) {
@@ -772,7 +791,10 @@ __global__ __launch_bounds__(SLICED ? kPickT : kAloneT) void sample_kernel(Sampl
 }
 
 // Slices of a row: a 16-byte piece or more for every thread, so many that the chip has some 1024 workgroups.
-constexpr int kAlone = 8192;
+// Rows of up to 16384 tokens, and of up to 65536 where there are 256 or more (a unit each): a workgroup a row (16384 fp32
+// logits, one row, greedy and top-50: 6.7 and 19 us, with slices 11.2 and 21; 256 rows of 32000: 8.6 and 31, 14 and 41; but
+// one row of 32000 bf16: 6.9 and 26, 11.5 and 22).
+bool alone(int64_t rows, int64_t V) { return V <= 16384 || (V <= 65536 && rows >= 256); }
 struct Slices {
   int n, tokens;
 };
@@ -787,7 +809,7 @@ Slices slices_of(int64_t rows, int64_t V, size_t elem) {
 template <typename T>
 catq_status launch_sample(SampleArgs a, int64_t rows, hipStream_t stream) {
   const double bytes = (double)rows * a.V * sizeof(T);
-  if (a.V <= kAlone) {
+  if (alone(rows, a.V)) {
     CATQ_TRACED(stream, "sample_kernel<alone>", 0.0, bytes, rows, a.V, 1,
                 hipLaunchKernelGGL((sample_kernel<T, false>), dim3((unsigned)rows), dim3(kAloneT), 0, stream, a));
     CATQ_CHECK_LAUNCH("sample");
@@ -816,7 +838,7 @@ catq_status launch_sample(SampleArgs a, int64_t rows, hipStream_t stream) {
 using namespace catq;
 
 extern "C" size_t catq_aux_sample_workspace_bytes(int64_t rows, int64_t V) {
-  if (rows <= 0 || rows > 65535 || V <= kAlone || V > (1 << 20)) return 0;
+  if (rows <= 0 || rows > 65535 || V > (1 << 20) || alone(rows, V)) return 0;
   return (size_t)rows * sizeof(RowSpace);
 }
 

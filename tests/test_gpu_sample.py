@@ -85,8 +85,8 @@ def _gen(seed):
     return g
 
 
-SIZES = [(1, 1, None), (3, 2, None), (5, 7, 9), (4, 100, None), (6, 1000, 1003), (3, 4097, None), (3, 8192, 8195), (3, 8193, None), (8, 32000, None),
-         (5, 50257, 50261), (4, 150000, None), (1, 262147, None), (70, 300, 301), (2, 1 << 20, None)]
+SIZES = [(1, 1, None), (3, 2, None), (5, 7, 9), (4, 100, None), (6, 1000, 1003), (3, 4097, None),
+         (3, 16384, 16389), (3, 16385, None), (8, 32000, None), (5, 50257, 50261), (4, 150000, None), (1, 262147, None), (70, 300, 301), (2, 1 << 20, None)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
@@ -102,6 +102,19 @@ def test_sample(catq, rows, V, ld, dtype):
                k=[int(v) for v in r.choice([1, 2, 40, 400, 5000, 2 ** 31 - 1], rows)] if on[0] else None,
                p=r.uniform(0.05, 0.999, rows) if on[1] else None, m=r.uniform(0.001, 0.3, rows) if on[2] else None,
                ld=ld, repeat=settings == 6)
+
+
+def test_sample_many_rows(catq):
+    """As many rows as the chip has units, each read by one workgroup."""
+    g = _gen(6)
+    n, V = 257, 40001
+    x = torch.randn((n, V), generator=g) * 2.5
+    x[:, 17] += 7
+    x[100:, V // 2:] = -math.inf
+    r = np.random.RandomState(1)
+    _check(catq, x, r.rand(n), ld=V + 1, repeat=False)
+    _check(catq, x.bfloat16(), r.rand(n), T=r.uniform(0.5, 1.2, n), k=[int(v) for v in r.choice([0, 30, 9000], n)],
+           p=r.uniform(0.3, 1.1, n), repeat=False)
 
 
 def test_sample_ties(catq):
