@@ -8,12 +8,16 @@
 // keep[i] >= i: a token moves down or stays, and what is read for one scale block lies in that block or behind
 // it.  A workgroup takes K or V of one kv head of a sequence and goes through its blocks in order: it reads a
 // window of tokens into registers, waits for all its waves, and writes them; nothing that it writes is read later
-// by it, and no other workgroup reads or writes these blocks.
+// by it, so the next window's reads are under way meanwhile, and no other workgroup reads or writes these blocks.
 // A block's scale becomes the largest of the scales that its tokens (the older ones too) come with, and codes that
 // come with another are rounded again: rne(code * (their scale / the block's)), half a step of the block's scale
 // at most.  With a scale per token (scale_block 1) nothing is rounded.
-// Up to 8 of 60 drafted tokens in each of 64 sequences, 8 heads of 128: 10 us, 1024 workgroups that each wait for lengths, list,
-// page, source page and codes in turn; one sequence: 4.5.
+// Up to 8 of 60 drafted tokens in each of 64 sequences, 8 heads of 128: 10 us, 1024 workgroups that each wait for
+// lengths, list, page, source page and codes in turn; one sequence: 4.5.  20000 of 30000 tokens in each of 4: 766 us,
+// 64 workgroups that each take 5 us for a window of 128 (with a window's loads not ahead and 32 tokens a window 3.5 us,
+// 2220 in all).
+#include <algorithm>
+
 #include "kv_common.h"
 #include "quant8.h"
 
@@ -67,14 +71,14 @@ struct CompactArgs {
   int32_t w_log2;       // tokens of a window
 };
 
-// Sixteen codes (one token's, of one lane) at a token of either array
-__device__ __forceinline__ u32x4 load_codes(const int8_t* p, bool is_v) {
-  if (!is_v) return *reinterpret_cast<const u32x4*>(p);
+// Sixteen codes of a token out of the array's words: of k as they stand, of v a byte of each of sixteen words
+__device__ __forceinline__ u32x4 token_codes(const u32x4 (&w)[4], int tok, bool is_v) {
+  if (!is_v) return w[0];
+  const unsigned pair = 0x0c0c0400u + 0x0101u * (unsigned)(tok & 3), high = (pair << 16) | 0x0c0cu;
   u32x4 r;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    r[j] = (unsigned)(uint8_t)p[16 * j] | ((unsigned)(uint8_t)p[16 * j + 4] << 8) |
-           ((unsigned)(uint8_t)p[16 * j + 8] << 16) | ((unsigned)(uint8_t)p[16 * j + 12] << 24);
+    r[j] = __builtin_amdgcn_perm(w[j][1], w[j][0], pair) | __builtin_amdgcn_perm(w[j][3], w[j][2], high);
   return r;
 }
 
@@ -95,8 +99,7 @@ template <int LPH, int NP>
 __global__ __launch_bounds__(256) void kv_compact_kernel(CompactArgs a) {
   constexpr int D = LPH * 16, TP = 256 / LPH;
   __shared__ int s_end;
-  __shared__ unsigned int s_mag[TP * NP];
-  __shared__ float s_scale[TP * NP];
+  __shared__ unsigned int s_mag[3][TP * NP];   // the blocks' largest scales: a window's, the next one's, cleared ones
   __shared__ __align__(16) unsigned char s_tile[TP * NP * D];
   const KvGeom& g = a.g;
   const int tid = threadIdx.x, sub = tid & (LPH - 1), tl = tid / LPH;
@@ -107,6 +110,7 @@ __global__ __launch_bounds__(256) void kv_compact_kernel(CompactArgs a) {
   const int32_t* keep = a.keep + q.row0;
   // the list ends before the first entry that does not rise or is no new token of the sequence
   if (tid == 0) s_end = want;
+  for (int i = tid; i < 3 * TP * NP; i += 256) s_mag[0][i] = 0u;
   __syncthreads();
   for (int i = tid; i < want; i += 256) {
     const int k = keep[i];
@@ -121,70 +125,116 @@ __global__ __launch_bounds__(256) void kv_compact_kernel(CompactArgs a) {
   int8_t* codes = is_v ? a.c.v : a.c.k;
   float* scales = is_v ? a.c.v_scale : a.c.k_scale;
   const int32_t* table = g.table + (int64_t)s * g.max_pages;
-  for (int64_t first = begin >> a.w_log2 << a.w_log2; first < end; first += W) {
-    const int tok0 = (int)(first & ps_mask);
-    const int lo = (int)max(begin - first, (int64_t)0), hi = (int)min(end - first, (int64_t)W);
-    const int old0 = lo & ~(bt - 1);      // tokens old0 .. lo - 1 of the window are the older ones of a block
-    const int page = table[first >> g.ps_log2];
-    const bool there = page >= 0 && page < g.n_pages;
-    // sources (those of a token without a page count as zeros)
-    u32x4 v[NP];
-    float sc[NP];
+  const int64_t begin_w = begin >> a.w_log2 << a.w_log2;
+  if (begin_w >= end) return;
+  // A window's tokens come through three loads in a row: their place in the list, its page, the codes.  Each is under way
+  // while the window before is written, from clamped addresses, and what does not count is dropped when it has come: no
+  // earlier window writes what a later one reads.
+  auto places = [&](int64_t first, int (&k)[NP]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      k[p] = keep[min(max(first + p * TP + tl - q.ctx, (int64_t)0), (int64_t)want - 1)];
+  };
+  auto page_at = [&](int64_t pos) __attribute__((always_inline)) {
+    return table[min(max(pos >> g.ps_log2, (int64_t)0), (int64_t)g.max_pages - 1)];
+  };
+  auto pages = [&](int64_t first, const int (&k)[NP], int64_t (&pos)[NP], int (&id)[NP]) __attribute__((always_inline)) {
+    const int lo = (int)max(begin - first, (int64_t)0), hi = (int)max(min(end - first, (int64_t)W), (int64_t)0);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int t = p * TP + tl;
-      v[p] = u32x4{0u, 0u, 0u, 0u};
-      sc[p] = 0.f;
-      if (there && t >= old0 && t < hi) {
-        const int64_t pos = t < lo ? first + t : (int64_t)q.ctx + keep[first + t - q.ctx];
-        const int from = pos < 0 || pos >= kv_capacity(g) ? -1 : table[pos >> g.ps_log2];
-        if (from >= 0 && from < g.n_pages) {
-          const int tok = (int)(pos & ps_mask);
-          const int64_t base = kv_code_base(g, from, h, is_v ? tok & ~3 : tok);
-          v[p] = load_codes(codes + base + (is_v ? 64 * sub + (tok & 3) : 16 * sub), is_v);
-          sc[p] = scales[kv_scale_index(g, from, h, tok)];
-        }
-      }
-      if (sub == 0 && t < W) s_mag[t] = mag_bits(sc[p]);
+      pos[p] = t < lo ? first + t : (int64_t)q.ctx + k[p];
+      if (t < (lo & ~(bt - 1)) || t >= hi || pos[p] >= kv_capacity(g)) pos[p] = -1;
+      id[p] = page_at(pos[p]);
     }
-    wait_vmem();
-    __syncthreads();   // everything that this window's writes could change has been read
+  };
+  auto load = [&](const int64_t (&pos)[NP], const int (&id)[NP], u32x4 (&w)[NP][4], float (&sc)[NP], int (&at)[NP])
+      __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const bool ok = pos[p] >= 0 && id[p] >= 0 && id[p] < g.n_pages;
+      const int page = ok ? id[p] : 0, tok = ok ? (int)(pos[p] & ps_mask) : 0;
+      at[p] = ok ? tok : -1;
+      const u32x4* from = reinterpret_cast<const u32x4*>(codes + kv_code_base(g, page, h, is_v ? tok & ~3 : tok)) +
+                          (is_v ? 4 * sub : sub);
+      w[p][0] = from[0];
+      if (is_v) {
+#pragma unroll
+        for (int j = 1; j < 4; ++j) w[p][j] = from[j];
+      }
+      sc[p] = scales[kv_scale_index(g, page, h, tok)];
+    }
+  };
+  int k[NP], id[NP], at[NP];
+  int lane0 = 0;       // (so that the window's own page is held a lane, not waited for to be held once)
+  asm volatile("" : "+v"(lane0));
+  int64_t pos[NP];
+  u32x4 w[NP][4];
+  float came[NP];
+  int page_next = page_at(begin_w + lane0);
+  places(begin_w, k);
+  pages(begin_w, k, pos, id);
+  places(begin_w + W, k);
+  load(pos, id, w, came, at);
+  pages(begin_w + W, k, pos, id);
+  places(begin_w + 2 * W, k);
+  int mine = 0;
+  for (int64_t first = begin_w; first < end; first += W, mine = mine == 2 ? 0 : mine + 1) {
+    const int tok0 = (int)(first & ps_mask);
+    const int lo = (int)max(begin - first, (int64_t)0), hi = (int)min(end - first, (int64_t)W);
+    const int old0 = lo & ~(bt - 1);      // tokens old0 .. lo - 1 of the window are the older ones of a block
+    const int page = __builtin_amdgcn_readfirstlane(page_next);
+    const bool there = page >= 0 && page < g.n_pages;
+    u32x4 v[NP];
+    float sc[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {        // (a token without a page counts as zeros)
+      v[p] = at[p] < 0 ? u32x4{0u, 0u, 0u, 0u} : token_codes(w[p], at[p], is_v);
+      sc[p] = at[p] < 0 ? 0.f : came[p];
+      const int t = p * TP + tl;
+      // (on the bits: a NaN is above all)
+      if (sub == 0 && t < W) atomicMax(&s_mag[mine][t >> g.bt_log2], mag_bits(sc[p]));
+    }
+    wait_vmem();       // everything that this window's writes could change has been read
+#pragma unroll
+    for (int p = 0; p < NP; ++p) asm volatile("" : "+v"(id[p]), "+v"(k[p]));
+    load(pos, id, w, came, at);
+    pages(first + 2 * W, k, pos, id);
+    places(first + 3 * W, k);
+    page_next = page_at(first + W + lane0);
+    __syncthreads();
     const int64_t cbase = kv_code_base(g, there ? page : 0, h, tok0);
     const int64_t sbase = kv_scale_index(g, there ? page : 0, h, tok0);
     for (int b = tid; b < (W >> g.bt_log2); b += 256) {
       const int t0 = b << g.bt_log2;
-      if (!there || t0 >= hi || t0 + bt <= lo) continue;
-      unsigned int m = 0u;       // (on the bits: a NaN is above all)
-      for (int i = 0; i < bt; ++i) m = max(m, s_mag[t0 + i]);
-      const float now = __uint_as_float(m);
-      s_scale[b] = now;
-      scales[sbase + b] = now;
+      s_mag[mine == 0 ? 2 : mine - 1][b] = 0u;   // the window before has read them, the one after the next fills them
+      if (there && t0 < hi && t0 + bt > lo) scales[sbase + b] = __uint_as_float(s_mag[mine][b]);
     }
-    __syncthreads();
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int t = p * TP + tl;
       if (!there || t < old0 || t >= hi) continue;
-      const float now = s_scale[t >> g.bt_log2];
+      const float now = __uint_as_float(s_mag[mine][t >> g.bt_log2]);
       if (now > sc[p]) v[p] = rescale(v[p], sc[p] / now);
       if (is_v) *reinterpret_cast<u32x4*>(s_tile + t * D + 16 * sub) = v[p];
       else *reinterpret_cast<u32x4*>(codes + cbase + (int64_t)t * D + 16 * sub) = v[p];
     }
-    if (!is_v) continue;
-    __syncthreads();
-    // words of four tokens at one d, whole ones at once and the others by bytes
-    for (int i = tid; there && i < (W >> 2) * D; i += 256) {
-      const int t4 = (i / D) * 4, dd = i % D;
-      if (t4 + 4 <= old0 || t4 >= hi) continue;
-      int8_t* dst = codes + cbase + (int64_t)t4 * D + dd * 4;
-      if (t4 >= old0 && t4 + 4 <= hi) {
-        *reinterpret_cast<unsigned int*>(dst) =
-            (unsigned)s_tile[t4 * D + dd] | ((unsigned)s_tile[(t4 + 1) * D + dd] << 8) |
-            ((unsigned)s_tile[(t4 + 2) * D + dd] << 16) | ((unsigned)s_tile[(t4 + 3) * D + dd] << 24);
-      } else {
+    if (is_v) {
+      __syncthreads();
+      // words of four tokens at one d, whole ones at once and the others by bytes
+      for (int i = tid; there && i < (W >> 2) * D; i += 256) {
+        const int t4 = (i / D) * 4, dd = i % D;
+        if (t4 + 4 <= old0 || t4 >= hi) continue;
+        int8_t* dst = codes + cbase + (int64_t)t4 * D + dd * 4;
+        if (t4 >= old0 && t4 + 4 <= hi) {
+          *reinterpret_cast<unsigned int*>(dst) =
+              (unsigned)s_tile[t4 * D + dd] | ((unsigned)s_tile[(t4 + 1) * D + dd] << 8) |
+              ((unsigned)s_tile[(t4 + 2) * D + dd] << 16) | ((unsigned)s_tile[(t4 + 3) * D + dd] << 24);
+        } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (t4 + k >= old0 && t4 + k < hi) dst[k] = (int8_t)s_tile[(t4 + k) * D + dd];
+          for (int k = 0; k < 4; ++k)
+            if (t4 + k >= old0 && t4 + k < hi) dst[k] = (int8_t)s_tile[(t4 + k) * D + dd];
+        }
       }
     }
   }
@@ -261,9 +311,9 @@ extern "C" catq_status catq_aux_kv_compact(const catq_kv_desc* d, const catq_kv_
   a.c = *cache;
   a.keep = keep;
   a.n_keep = n_keep;
-  // a window lies in one page and holds whole scale blocks
-  const int tp = 256 / (d->head_dim / 16);
-  const int w = d->scale_block > tp ? d->scale_block : (tp < d->page_size ? tp : d->page_size);
+  // A window lies in one page and holds whole scale blocks; up to four passes of the threads (one pass: 984 us where
+  // four take 766, and the same for a few tokens).
+  const int w = std::max(d->scale_block, std::min(std::min(4 * 256 / (d->head_dim / 16), 128), d->page_size));
   a.w_log2 = __builtin_ctz((unsigned)w);
   switch (d->head_dim) {
     case 64: return launch_compact<4>(a, stream);

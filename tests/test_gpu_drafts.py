@@ -354,6 +354,11 @@ COMPACT = [
     ([(0, 300), (33, 200)], 2, 64, 16, 16, [list(range(1, 300, 2)), list(range(100, 200))]),
     ([(0, 300)], 2, 128, 64, 1, [[i for i in range(300) if i % 7 != 3]]),
     ([(20, 100)], 1, 256, 256, 128, [[i for i in range(100) if i % 3]]),
+    # many windows, pages and passes
+    ([(77, 900), (0, 513)], 2, 128, 128, 32, [[i for i in range(900) if i % 5 != 1], list(range(513))]),
+    ([(130, 700)], 1, 64, 256, 16, [list(range(350, 700))]),
+    ([(3, 600)], 1, 256, 64, 1, [[i for i in range(600) if i % 2]]),
+    ([(200, 600)], 1, 256, 128, 128, [[i for i in range(600) if i % 4 != 2]]),
     # lists that end early: repeated, falling, out of range
     ([(5, 9), (17, 8), (3, 4), (2, 6)], 2, 64, 32, 16, [[0, 3, 3, 8], [4, 2, 7], [-1, 2], [1, 6]]),
 ]
