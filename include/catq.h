@@ -624,7 +624,7 @@ catq_status catq_aux_kv_compact(const catq_kv_desc* d, const catq_kv_cache* cach
  * w = exp((logit - largest) / temperature).  Kept are, one filter after the other,
  *   top_k   the first top_k tokens (<= 0: all)
  *   top_p   of these, those before which less than top_p of their weight lies (>= 1: all; the first always)
- *   min_p   of these, those with w >= min_p (<= 0: all; the first always)
+ *   min_p   of these, those with w >= min_p (<= 0: all; the first always, and alone above 1)
  * and the row's token is the lowest index up to which the kept tokens of lower or equal index hold more than
  * u of the kept weight; prob (NULL: not written) is its share of that.
  *   temperature, top_p, min_p, u  fp32 [rows];  top_k  int32 [rows];  token  int32 [rows]; prob  fp32 [rows]

@@ -83,7 +83,7 @@ __device__ __forceinline__ Settings settings(const SampleArgs& a, int64_t row) {
   p.top_p = a.top_p ? a.top_p[row] : 1.0f;
   p.min_p = a.min_p ? a.min_p[row] : 0.0f;
   p.top_k = a.top_k ? a.top_k[row] : 0;
-  p.first_only = !(p.temp > 0.0f) || p.top_k == 1 || p.top_p <= 0.0f;
+  p.first_only = !(p.temp > 0.0f) || p.top_k == 1 || p.top_p <= 0.0f || p.min_p > 1.0f;   // (no weight is above 1)
   p.filtered = p.top_k > 0 || p.top_p < 1.0f;
   return p;
 }
@@ -113,9 +113,9 @@ __device__ __forceinline__ Row row_of(u64 first, float temp) {
   r.bins = fminf(64.0f / temp, 1e30f);
   return r;
 }
-// the least exponent that min-p keeps
+// the least exponent that a min-p of at most 1 keeps
 __device__ __forceinline__ double least_of(float min_p) {
-  return min_p > 0.0f ? fmin(log2((double)min_p), 0.0) : -INFINITY;
+  return min_p > 0.0f ? log2((double)min_p) : -INFINITY;
 }
 // (logit - largest) log2(e) / temperature, off by 2^-53 of the larger product; equal ones give 0 also where both
 // are infinite

@@ -226,3 +226,32 @@ def test_sample_captured_and_on_another_stream(catq):
     step(side.cuda_stream)
     side.synchronize()
     assert torch.equal(token, want[0][0]) and torch.equal(prob, want[0][1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,ld", [(4, 1000, 1003), (5, 40000, 40001), (3, 150000, None), (256, 40000, 40001)])
+def test_sample_min_p_and_tied_logits(catq, rows, V, ld, dtype):
+    """No weight is above 1: a min_p of 1 keeps all tokens that tie with the largest logit, one above it the first of them
+    alone, with every filter beside it."""
+    x = (torch.randn((rows, V), generator=_gen(V)) * 2).to(dtype)
+    x[:, [5, V // 2, V - 1]] = 20.0
+    x[1, [17, V // 3, V - 2]] = math.inf
+    x[2] = 1.0
+    first = torch.full((rows,), 5, dtype=torch.int32)
+    first[1], first[2] = 17, 0
+    T = [(0.5, 1.0, 2.0)[r % 3] for r in range(rows)]
+    above = [(1.5, 1 + 2.0 ** -23, 3e38, math.inf)[r % 4] for r in range(rows)]
+    dev = torch.full((rows, ld or V), 1e4, dtype=dtype, device="cuda")[:, :V]
+    dev.copy_(x)
+    f = lambda v, dt=torch.float32: None if v is None else torch.tensor([v] * rows, dtype=dt, device="cuda")  # noqa: E731
+    ws = torch.empty(max(16, catq.catq_aux_sample_workspace_bytes(rows, V)), dtype=torch.uint8, device="cuda")
+    for k, p in ((None, None), (50, None), (None, 0.7), (50, 0.7), (2, 0.9), (5000, 0.99)):
+        for u in (0.0, 0.5, 0.9, 0.999):
+            token = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+            prob = torch.full((rows,), -7.0, device="cuda")
+            catq.catq_aux_sample(dev, f(u), token, ws, temperature=torch.tensor(T, device="cuda"), top_k=f(k, torch.int32),
+                                 top_p=f(p), min_p=torch.tensor(above, device="cuda"), prob=prob)
+            assert torch.equal(token.cpu(), first) and (prob == 1.0).all(), (k, p, u)
+    for k, p in ((None, None), (2, None), (None, 0.7), (50, 0.7)):
+        _check(catq, x[:3], [0.4, 0.6, 0.9], T=T[:3], k=None if k is None else [k] * 3, p=None if p is None else [p] * 3,
+               m=[1.0, 1.0, 1.0], ld=ld, repeat=False)
