@@ -632,8 +632,8 @@ catq_status catq_aux_kv_compact(const catq_kv_desc* d, const catq_kv_cache* cach
  * temperature that is not above 0 takes the first token, with prob 1.  A NaN in top_p or min_p leaves that filter out.
  * A logit that is NaN or -inf is never taken; where a row has no other, token is -1 and prob 0.  +inf logits share the
  * whole weight.  Weights are held to 2^-43 of the largest, in integers: the result is the same every time.  The
- * workspace (at least catq_aux_sample_workspace_bytes(rows, V) bytes; 0: may be NULL) is for one call at a time.
- * logits and workspace 16-byte aligned, the others 4-byte.
+ * workspace (at least catq_aux_sample_workspace_bytes(rows, V) bytes, which serve calls of fewer rows or tokens too; 0: may
+ * be NULL) is for one call at a time.  logits and workspace 16-byte aligned, the others 4-byte.
  */
 size_t catq_aux_sample_workspace_bytes(int64_t rows, int64_t V);
 catq_status catq_aux_sample(const void* logits, catq_dtype dtype, int64_t rows, int64_t V, int64_t ld,

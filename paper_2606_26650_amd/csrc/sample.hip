@@ -794,7 +794,10 @@ __global__ __launch_bounds__(SLICED ? kPickT : kAloneT) void sample_kernel(Sampl
 // Rows of up to 16384 tokens, and of up to 65536 where there are 256 or more (a unit each): a workgroup a row (16384 fp32
 // logits, one row, greedy and top-50: 6.7 and 19 us, with slices 11.2 and 21; 256 rows of 32000: 8.6 and 31, 14 and 41; but
 // one row of 32000 bf16: 6.9 and 26, 11.5 and 22).
-bool alone(int64_t rows, int64_t V) { return V <= 16384 || (V <= 65536 && rows >= 256); }
+constexpr int64_t kAloneRows = 256;
+bool alone(int64_t rows, int64_t V) { return V <= 16384 || (V <= 65536 && rows >= kAloneRows); }
+// What the call itself needs
+size_t space_of(int64_t rows, int64_t V) { return alone(rows, V) ? 0 : (size_t)rows * sizeof(RowSpace); }
 struct Slices {
   int n, tokens;
 };
@@ -838,8 +841,9 @@ catq_status launch_sample(SampleArgs a, int64_t rows, hipStream_t stream) {
 using namespace catq;
 
 extern "C" size_t catq_aux_sample_workspace_bytes(int64_t rows, int64_t V) {
-  if (rows <= 0 || rows > 65535 || V > (1 << 20) || alone(rows, V)) return 0;
-  return (size_t)rows * sizeof(RowSpace);
+  if (rows <= 0 || rows > 65535 || V > (1 << 20)) return 0;
+  // (enough for fewer rows too, which may be read by several workgroups each where so many are not)
+  return space_of(alone(rows, V) ? std::min(rows, kAloneRows - 1) : rows, V);
 }
 
 extern "C" catq_status catq_aux_sample(const void* logits, catq_dtype dtype, int64_t rows, int64_t V, int64_t ld,
@@ -858,7 +862,7 @@ extern "C" catq_status catq_aux_sample(const void* logits, catq_dtype dtype, int
   CATQ_REQUIRE(aligned16(logits) && at4(temperature) && at4(top_k) && at4(top_p) && at4(min_p) && at4(u) &&
                    at4(token) && at4(prob) && aligned16(workspace),
                CATQ_ERR_ALIGN, "logits and workspace must be 16-byte aligned, the others 4-byte");
-  const size_t need = catq_aux_sample_workspace_bytes(rows, V);
+  const size_t need = space_of(rows, V);
   CATQ_REQUIRE(need == 0 || (workspace && workspace_bytes >= need), CATQ_ERR_WORKSPACE,
                "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : (size_t)0);
   const SampleArgs a{logits, ld, (int32_t)V, temperature, top_k, top_p, min_p, u, token, prob,

@@ -120,6 +120,19 @@ def test_sample_refusals(cq):
     assert cq.catq_aux_sample_workspace_bytes(0, 5) == 0 and cq.catq_aux_sample_workspace_bytes(-1, -1) == 0
 
 
+def test_sample_workspace_serves_fewer_rows(cq):
+    """A program sizes its workspace once, for its largest batch: the size never falls as rows (or the vocabulary) rise."""
+    need = cq.catq_aux_sample_workspace_bytes
+    rows = [1, 2, 64, 254, 255, 256, 257, 300, 1024, 1025, 65535]
+    for V in (1, 16384, 16385, 32000, 65536, 65537, 150000, 1 << 20):
+        sizes = [need(r, V) for r in rows]
+        assert sizes == sorted(sizes), V
+    for r in rows:
+        sizes = [need(r, V) for V in (1, 16384, 16385, 65536, 65537, 1 << 20)]
+        assert sizes == sorted(sizes), r
+    assert need(65536, 32000) == 0 and need(5, (1 << 20) + 1) == 0 and need(5, 0) == 0
+
+
 def test_moe_refusals(cq):
     ok = dict(E=8, k=2, h=256, F=128, g=128, x=FAKE, q=FAKE, T=4, ld=256, xs=FAKE, P1=FAKE, A1=FAKE, P2=FAKE, A2=FAKE,
               res=FAKE, y=FAKE, dt=1, ws=FAKE, n=1 << 40)

@@ -255,3 +255,24 @@ def test_sample_min_p_and_tied_logits(catq, rows, V, ld, dtype):
     for k, p in ((None, None), (2, None), (None, 0.7), (50, 0.7)):
         _check(catq, x[:3], [0.4, 0.6, 0.9], T=T[:3], k=None if k is None else [k] * 3, p=None if p is None else [p] * 3,
                m=[1.0, 1.0, 1.0], ld=ld, repeat=False)
+
+
+@pytest.mark.parametrize("V", [20000, 65536, 66000])
+def test_sample_one_workspace_for_fewer_rows(catq, V):
+    """The workspace of the largest batch serves every smaller one; rows that a workgroup reads alone need none."""
+    most = 300
+    x = (torch.randn((most, V), generator=_gen(V)) * 2.5).bfloat16().cuda()
+    u = torch.rand(most, generator=_gen(1)).cuda()
+    top_p = torch.full((most,), 0.8, device="cuda")
+    ws = torch.empty(catq.catq_aux_sample_workspace_bytes(most, V), dtype=torch.uint8, device="cuda")
+    for n in (most, 256, 255, 9, 1):
+        own = torch.empty(max(16, catq.catq_aux_sample_workspace_bytes(n, V)), dtype=torch.uint8, device="cuda")
+        spaces = [ws, own] + ([None] if n >= 256 and V <= 65536 else [])
+        got = []
+        for w in spaces:
+            token, prob = torch.full((n,), -7, dtype=torch.int32, device="cuda"), torch.full((n,), -7.0, device="cuda")
+            catq.catq_aux_sample(x[:n], u[:n], token, w, top_p=top_p[:n], prob=prob)
+            assert (token >= 0).all() and (prob > 0).all()
+            got.append((token, prob))
+        for token, prob in got[1:]:
+            assert torch.equal(token, got[0][0]) and torch.equal(prob, got[0][1])
