@@ -570,12 +570,13 @@ typedef struct {
                              bit is set).  Bits past the sequence's new tokens are ignored  */
   const int32_t* depth;   /* [n_tokens]: the row's k and q turn by position ctx_len[s] + depth; NULL
                              for ctx_len[s] + i                                        */
-  int32_t words;          /* at least max_new / 64 rounded up, at most 1024            */
+  int32_t words;          /* at least max_new / 64 rounded up, at most 1024; without a mask
+                             not looked at                                              */
 } catq_kv_tree;           /* mask 8-byte aligned, depth 4-byte                          */
 
 /*
  * catq_aux_kv_append_tree: catq_aux_kv_append with each token rotated for the depth it has in
- * the tree (mask is not read and may be NULL).
+ * the tree (mask is not read and may be NULL; then it takes as many new tokens as catq_aux_kv_append).
  * catq_aux_tree_attention: catq_aux_paged_attention where row i of sequence s sees every
  * position before ctx_len[s], and of the new tokens those that its mask names.  The depth is not
  * read.  A row that sees nothing (an empty mask behind no cached token) gives o = 0 and lse =

@@ -75,9 +75,9 @@ catq_status kv_check(const catq_kv_desc* d, const catq_kv_cache* c, const catq_k
   return CATQ_OK;
 }
 
-catq_status kv_check_tree(const catq_kv_batch* b, const catq_kv_tree* t) {
+catq_status kv_check_tree(const catq_kv_batch* b, const catq_kv_tree* t, bool masked) {
   CATQ_REQUIRE(t, CATQ_ERR_NULL, "tree must not be NULL");
-  CATQ_REQUIRE(t->words > 0 && t->words <= 1024 && (int64_t)t->words * 64 >= b->max_new, CATQ_ERR_SHAPE,
+  CATQ_REQUIRE(!masked || (t->words > 0 && t->words <= 1024 && (int64_t)t->words * 64 >= b->max_new), CATQ_ERR_SHAPE,
                "a mask row needs 64-bit words for max_new tokens, and has at most 1024");
   CATQ_REQUIRE((reinterpret_cast<uintptr_t>(t->mask) & 7) == 0 && (reinterpret_cast<uintptr_t>(t->depth) & 3) == 0,
                CATQ_ERR_ALIGN, "mask must be 8-byte aligned, depth 4-byte");
@@ -586,7 +586,7 @@ extern "C" catq_status catq_aux_kv_append_tree(const catq_kv_desc* d, const catq
                                                hipStream_t stream) {
   clear_error();
   CATQ_TRY(kv_check(d, cache, batch));
-  CATQ_TRY(kv_check_tree(batch, tree));
+  CATQ_TRY(kv_check_tree(batch, tree, tree && tree->mask));   // (the mask is not read: without one any number of tokens)
   return append(d, cache, batch, tree->depth, prep, qkv, q_out, stream);
 }
 

@@ -49,7 +49,8 @@ __device__ __forceinline__ int64_t kv_scale_index(const KvGeom& g, int page, int
 
 catq_status kv_check_desc(const catq_kv_desc* d);
 catq_status kv_check_pool(const catq_kv_desc* d, const catq_kv_cache* c);
-catq_status kv_check_tree(const catq_kv_batch* b, const catq_kv_tree* t);
+// masked: the mask has to hold a bit for every new token
+catq_status kv_check_tree(const catq_kv_batch* b, const catq_kv_tree* t, bool masked);
 catq_status kv_check(const catq_kv_desc* d, const catq_kv_cache* c, const catq_kv_batch* b);
 catq_status kv_check_sizes(const catq_kv_desc* d, const catq_kv_batch* b);
 KvGeom kv_geom(const catq_kv_desc* d, const catq_kv_batch* b);

@@ -1052,6 +1052,6 @@ extern "C" catq_status catq_aux_tree_attention(const catq_kv_desc* d, const catq
                                                void* workspace, size_t workspace_bytes, hipStream_t stream) {
   clear_error();
   CATQ_TRY(kv_check(d, cache, batch));
-  CATQ_TRY(kv_check_tree(batch, tree));
+  CATQ_TRY(kv_check_tree(batch, tree, true));
   return attend(d, cache, batch, tree, q, scale, o, lse, workspace, workspace_bytes, stream);
 }

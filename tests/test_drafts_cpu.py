@@ -66,6 +66,28 @@ def test_tree_refusals(cq):
     assert both(n=need - 1, **long)[1] == WORKSPACE and both(ws=None, **long)[1] == WORKSPACE
 
 
+def test_append_by_depth_alone_has_no_mask_limits(cq):
+    """The append of a tree does not read the mask: without one its words are not looked at, and as many new tokens are
+    taken as by the plain append (no tokens here, so nothing is launched)."""
+    L = cq.lib
+    big = dict(n_tokens=0, max_new=70000, max_pages=2000, n_pages=2000, max_len=100000)
+
+    def append(qkv=FAKE, **kw):
+        d, c, b, p, t = _structs(cq, **dict(big, **kw))
+        return L.catq_aux_kv_append_tree(R(d), R(c), R(b), R(t), R(p), qkv, FAKE, None)
+
+    for words in (1094, 1024, 1, 0, -1):
+        assert append(mask=None, words=words) == 0, words
+        assert append(mask=None, depth=None, words=words) == 0, words
+    assert append(mask=None, max_new=1 << 24) == 0 and append(mask=None, max_new=(1 << 24) + 1) == SHAPE
+    assert append(mask=None, depth=FAKE + 2) == ALIGN
+    assert append(words=1024) == SHAPE and append(words=1094) == SHAPE       # (a mask, too long for the attention)
+    d, c, b, p, t = _structs(cq, **big, mask=None, words=1)
+    assert L.catq_aux_tree_attention(R(d), R(c), R(b), R(t), FAKE, 0.1, FAKE, None, None, 0, None) == SHAPE
+    b.device = -1
+    assert cq.kv_tree(b).words == 1094
+
+
 def test_page_refusals(cq):
     L = cq.lib
 

@@ -267,6 +267,24 @@ def test_append_tree_of_a_chain(catq):
     assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
 
 
+def test_append_tree_of_a_long_chain(catq):
+    """More new tokens than a mask has bits for: by their depths alone the append takes what the plain one takes."""
+    n, out = 70001, []
+    for kind in range(3):
+        sv = Serving(catq, [(9, n)], 1, 1, 64, 256, 16).upload()
+        x = _rand(_gen(2), n, 3 * 64).cuda()
+        prep = catq.kv_prep(sv.desc, (1e4 ** (-torch.arange(32) / 32)).float().cuda(), rot_dim=64)
+        q = torch.full((n, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+        if kind == 0:
+            catq.catq_aux_kv_append(sv.desc, sv.cache, sv.batch, prep, x, q)
+        else:
+            tree = catq.kv_tree(sv.batch, depth=torch.arange(n, dtype=torch.int32, device="cuda") if kind == 1 else None)
+            catq.catq_aux_kv_append_tree(sv.desc, sv.cache, sv.batch, tree, prep, x, q)
+        out.append([q] + sv.dev)
+    for a, b, c in zip(*out):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
 # ------------------------------------------------------------------------ pages
 
 @pytest.mark.parametrize("n_kv,d,ps,bt", [(1, 64, 16, 16), (3, 64, 16, 1), (8, 128, 64, 16), (2, 256, 256, 128),
