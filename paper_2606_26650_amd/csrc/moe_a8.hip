@@ -10,12 +10,15 @@
 //
 // Launches.  One token: every wave of the first kernel finds its experts itself, every workgroup of the second forms the
 // codes of a: two launches.  More tokens: the experts and their slots are laid out by a kernel of their own (in the first
-// kernel, two tokens took as long, four 54 us instead of 49.5), and so are the codes where they are more than LDS takes.
+// kernel, two tokens took as long, four 54 us instead of 49.5).  Where the codes are more than LDS takes (24 KB, and
+// from 9 tokens on), a kernel forms them, for one token too.
 //
 // What bounds it, 128 experts of 4096 x 1536, 8 a token: at one token (21 us, 42 MB) chains of latencies, routing 4 of the first
-// kernel's 12 us, codes 2 of the second's 10. At 32 tokens (147 us, 111 experts, 520 MB, 3.6 TB/s) HBM and the vector ALU
+// kernel's 12 us, codes 2 of the second's 10. At 32 tokens (147 us, 111 experts, 594 MB, 4.0 TB/s) HBM and the vector ALU
 // (54% of the issue in the first kernel, 42 in the second): of the instructions of a chunk of 16 rows 22 decode, 4 scale, 12 read
 // and address; with the activations as columns, in plain order and loaded for all of them, it took 221 us.
+// From 64 tokens on (215 us, where the weights read once take 130) the down kernel's weights, read again for every 32
+// tokens: 322 us at 128 tokens, 2095 at 1024.
 #include <type_traits>
 
 #include "kernels.h"

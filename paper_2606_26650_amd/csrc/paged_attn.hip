@@ -903,8 +903,9 @@ __global__ __launch_bounds__(256) void tree_join_kernel(PaArgs a) {
 // max_len: one sequence of 131072 tokens among 63 of 500 is walked in one span (1391 us; 50 and 17
 // in calls of their own), and 63 single tokens after 4000 beside a chunk of 2000 take its tiles
 // (904 us; 94 and 81). Heads of 256 have tiles of at most 32 rows: 256 values a row do not fit the
-// registers of the other kernel, and those of this one spill 13-18 (1000 tokens after 1000, 16 + 4
-// heads: 105 us, where a kernel at the rate of the products would take 17).
+// registers of the other kernel, and those of this one spill 14-18, 21-26 for trees (1000 tokens after 1000, 16 + 4
+// heads: 105 us, where a kernel at the rate of the products would take 17; trees of 60 after up to 4000 in 8
+// sequences: 122 and 9).
 struct Plan {
   int tile_rows, row_tiles, spans, span;
 };
